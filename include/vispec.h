@@ -21,6 +21,11 @@
  *   vispec_accept_sampled    acceptance at temperature > 0 (Sec. 3.1's min(1, p/p^) rule with residual resampling)
  *   vispec_cache_register_paged and the *_paged calls: the same work on a pool of cache blocks and a block table
  *
+ * and the steps around the prompt that the sequences start from:
+ *
+ *   vispec_rope_axes_rows    rotary embedding of packed q and k rows by several position axes (time, height, width)
+ *   vispec_kv_append         a ragged batch of new tokens' k/v rows, rotated on the way, into the cache
+ *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless its comment says "host".  The library never takes
  *     ownership of caller memory and never frees it.
@@ -109,11 +114,11 @@ typedef enum vispec_option {
      * read, and everything is written, only after it has completed.  Attention calls (and the stream probe) let
      * their successor start as soon as they have started themselves, so through a run of back-to-back attention
      * calls the early reads of a later call may overlap the kernel that preceded the first of them.  The rule:
-     * a kernel that writes kv_len or committed cache slots (vispec_kv_compact, vispec_accept_commit) must be
+     * a kernel that writes kv_len or committed cache slots (vispec_kv_compact, vispec_accept_commit, vispec_kv_append) must be
      * followed by at least one kernel that waits for its predecessor before it lets its successor in - any ordinary
      * kernel, or any call of this library other than the attention calls and the stream probe (they are all launched
-     * early, but wait first: vispec_tree_mask_build, vispec_rope_tree_rows, vispec_rope_table_build,
-     * vispec_tree_rerank, the acceptances, the commits) - before the next attention call with this option on; the
+     * early, but wait first: vispec_tree_mask_build, vispec_rope_tree_rows, vispec_rope_axes_rows, vispec_rope_table_build,
+     * vispec_tree_rerank, the acceptances, the commits, the appends) - before the next attention call with this option on; the
      * decoding cycle (commit, mask build, attention x layers) satisfies it.  Otherwise set 0 for the attention calls in between: then nothing is read early. */
     VISPEC_OPT_EARLY_PREFETCH = 1,
     /* Default 0 (1 if the environment has VISPEC_FORCE_GENERIC=1 at context creation).  Route attention
@@ -296,6 +301,59 @@ int vispec_rope_tree_rows_paged(vispec_ctx* ctx, int layer, void* q, const void*
  * Host errors: E_NULL, E_ALIGN (16 B), E_SHAPE, E_RANGE (layer), E_UNREGISTERED. */
 int vispec_rope_tree_rows(vispec_ctx* ctx, int layer, void* q, const void* k_new, const void* v_new,
                           const int32_t* positions, const int32_t* kv_len, int B, int N, float theta, void* stream);
+
+/* Rotary positions with several axes (Sec. 3.2: the target LLM is unchanged; Qwen2.5-VL gives the tokens of an image or a
+ * video a time, a height and a width position, and each frequency of the rotation belongs to one of them).  A host struct. */
+#define VISPEC_MAX_ROPE_AXES 4
+typedef struct vispec_rope_axes {
+    int32_t n_axes;                             /* 1..4; 1 is the ordinary rotation */
+    int32_t sections[VISPEC_MAX_ROPE_AXES];     /* frequencies per axis, each >= 1 up to n_axes, D/2 in all; rest ignored */
+    int32_t interleaved;                        /* 0: axis 0 has the first sections[0] frequencies, axis 1 the next, ...;
+                                                   1: frequency j belongs to axis j mod n_axes while j < n_axes *
+                                                   sections[j mod n_axes], to axis 0 otherwise (each axis has to come out
+                                                   with its section's number) */
+    float theta;                                /* rotary base, > 1 */
+} vispec_rope_axes;
+
+/* Rotary embedding of T packed tokens' q and k rows (vispec_rope_tree_rows' pairing, element j with element j + D/2):
+ *   angle(t, j) = positions[axis of j][t] * theta^(-2j/D),   j < D/2
+ * q [T,Hq,D], k [T,Hkv,D] bf16 with tokens q_stride / k_stride elements apart and a token's heads contiguous (slices of a
+ * fused projection's rows), positions [n_axes,T] int32.  q_out / k_out: the same layout with strides of their own; an output may
+ * be its input (then with the input's stride) but must not overlap it, or another argument, in any other way.  q with q_out,
+ * or k with k_out, may be NULL: those rows are not processed.  Angles are reduced in fp64, sines and products are fp32, one
+ * rounding to bf16.  T = 0 does nothing.
+ * Host errors: E_NULL (also both pairs NULL, one half of a pair NULL), E_ALIGN (pointers 16 B, strides multiples of 8),
+ * E_SHAPE (T < 0, a stride below the row, theta <= 1, sections that do not fit D/2, in place with another stride), E_CUDA. */
+int vispec_rope_axes_rows(vispec_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const int32_t* positions, int T, const vispec_rope_axes* axes /*host*/, void* q_out,
+                          int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/* New tokens' rows into the cache, rotated on the way: prompts, parts of prompts, or one token per running sequence (the paper
+ * has only App. A's pre-allocated cache; this fills it).  The batch is ragged and packed: sequence b owns tokens
+ * [cu_len[b], cu_len[b+1]) of the T rows, which go to its logical slots kv_len[b] + 0, 1, ...:
+ *   k_new [T,Hkv,D] (stride k_stride) rotated by positions [n_axes,T] and axes as in vispec_rope_axes_rows, written to the cache;
+ *   v_new [T,Hkv,D] (v_stride) copied;  q [T,Hq,D] (q_stride) rotated to q_out (q itself, or apart; both may be NULL);
+ *   kv_len_out[b] = kv_len[b] + cu_len[b+1] - cu_len[b]  (may be NULL; must not alias kv_len: E_SHAPE).
+ * axes NULL: no rotation, k is copied; then q, q_out and positions must be NULL.
+ * cu_len [B+1], kv_len [B] int32 (device).  Rows behind cu_len[B] (a batch padded to T) are not used, their q_out rows
+ * keep their bytes.  A sequence whose rows do not fit (kv_len < 0, or beyond the capacity) is left alone, kv_len_out[b] and
+ * its q_out rows included, with status word VISPEC_E_RANGE; a cu_len that decreases, starts below 0 or ends beyond T drops
+ * the whole call, with the same code.  All other slots keep their bytes.  One launch.  The call writes committed slots and kv_len_out:
+ * for the attention calls after it the rule of VISPEC_OPT_EARLY_PREFETCH applies as for a commit.
+ * Host errors: E_NULL, E_ALIGN, E_SHAPE (B outside [0, B_max] or above 8192, T < 0, strides, axes), E_RANGE (layer),
+ * E_UNREGISTERED, E_UNSUPPORTED (paged layer), E_CUDA. */
+int vispec_kv_append(vispec_ctx* ctx, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                     const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes /*host*/,
+                     const int32_t* cu_len, const int32_t* kv_len, int B, int T, void* q_out, int64_t q_out_stride,
+                     int32_t* kv_len_out, void* stream);
+/* The same on a paged layer: slots are found through block_table [B,table_stride] (capacity table_stride * page_rows); a
+ * table entry outside the pool drops that row's k and v and sets the status word VISPEC_E_RANGE.  E_UNSUPPORTED for a
+ * contiguous layer. */
+int vispec_kv_append_paged(vispec_ctx* ctx, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                           const void* v_new, int64_t v_stride, const int32_t* positions,
+                           const vispec_rope_axes* axes /*host*/, const int32_t* cu_len, const int32_t* kv_len,
+                           const int32_t* block_table, int table_stride, int B, int T, void* q_out, int64_t q_out_stride,
+                           int32_t* kv_len_out, void* stream);
 
 /* Measurement aid (the paper has no counterpart): reads exactly the K and V rows that
  * vispec_tree_verify_attn(layer, ..., kv_len, B, N) reads - slots [0, kv_len[b] + N) of every kv head, rounded

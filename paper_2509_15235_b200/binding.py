@@ -32,6 +32,7 @@ EXPORTS = [
     "vispec_cache_register_paged", "vispec_tree_verify_attn_paged", "vispec_kv_compact_paged",
     "vispec_accept_commit_paged", "vispec_rope_tree_rows_paged", "vispec_selftest_bounded_wait",
     "vispec_rope_table_build", "vispec_rope_table_bytes", "vispec_tree_verify_attn_rope",
+    "vispec_rope_axes_rows", "vispec_kv_append", "vispec_kv_append_paged",
 ]
 OPT_EARLY_PREFETCH = 1
 OPT_FORCE_GENERIC = 2
@@ -42,6 +43,23 @@ OPT_CHECK_POSITIONS = 5
 
 class VispecShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B_max", "N_max", "Hq", "Hkv", "D", "S_max", "layers")]
+
+
+class _RopeAxes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32),
+                ("theta", ctypes.c_float)]
+
+
+class RopeAxes:
+    """vispec_rope_axes: which position axis each of the D/2 rotary frequencies follows.  ``sections`` are the axes' numbers of
+    frequencies, in blocks or, with ``interleaved``, dealt in turn; one section is the ordinary rotation."""
+
+    def __init__(self, sections, theta: float, interleaved: bool = False):
+        self.sections, self.theta, self.interleaved = tuple(int(n) for n in sections), float(theta), bool(interleaved)
+        if not 1 <= len(self.sections) <= 4:
+            raise ValueError("one to four axes")
+        self._c = _RopeAxes(len(self.sections), (ctypes.c_int32 * 4)(*self.sections), int(self.interleaved), self.theta)
+        self._addr = ctypes.addressof(self._c)
 
 
 class VispecError(RuntimeError):
@@ -63,7 +81,7 @@ def load() -> ctypes.CDLL:
                 raise ImportError(f"{path} is missing: run `python -m paper_2509_15235_b200.build` "
                                   "(there is no fallback path)")
         lib = ctypes.CDLL(LIB_PATH)
-        vp, ci, cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_float
+        vp, ci, cf, cl = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int64
         lib.vispec_strerror.restype = ctypes.c_char_p
         lib.vispec_strerror.argtypes = [ci]
         sigs = {
@@ -93,6 +111,10 @@ def load() -> ctypes.CDLL:
             "vispec_rope_table_build": [vp, vp, ci, ci, cf, vp, vp],
             "vispec_rope_table_bytes": [vp, ci, ci, ctypes.POINTER(ctypes.c_size_t)],
             "vispec_tree_verify_attn_rope": [vp, ci, vp, vp, vp, vp, vp, vp, ci, ci, cf, vp, vp, vp],
+            "vispec_rope_axes_rows": [vp, vp, cl, vp, cl, vp, ci, ctypes.POINTER(_RopeAxes), vp, cl, vp, cl, vp],
+            "vispec_kv_append": [vp, ci, vp, cl, vp, cl, vp, cl, vp, ctypes.POINTER(_RopeAxes), vp, vp, ci, ci, vp, cl, vp, vp],
+            "vispec_kv_append_paged": [vp, ci, vp, cl, vp, cl, vp, cl, vp, ctypes.POINTER(_RopeAxes), vp, vp, vp, ci, ci, ci,
+                                       vp, cl, vp, vp],
             "vispec_tree_verify_attn_static": [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp],
         }
         for name, argtypes in sigs.items():
@@ -153,6 +175,7 @@ class VerifyContext:
         h = ctypes.c_void_p()
         _check(self.lib.vispec_ctx_create(ctypes.byref(h), ctypes.byref(self.shape), device), "vispec_ctx_create")
         self.handle = h
+        self._heads = (Hq, Hkv, D)
         self._h = h.value or 0          # the handle as the native calls take it
         n = ctypes.c_size_t()
         _check(self.lib.vispec_workspace_bytes(self.handle, ctypes.byref(n)), "vispec_workspace_bytes")
@@ -277,6 +300,27 @@ class VerifyContext:
         _check(_native.tree_verify_attn_rope(self._h, layer, q, k_new, v_new, rope_table, kv_len, tree_mask, scale, out,
                                              lse),
                "vispec_tree_verify_attn_rope")
+
+    def rope_axes_rows(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, axes: RopeAxes,
+                       q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor]) -> None:
+        """Rows [T, heads, D] whose tokens may be any stride apart (slices of a fused projection); positions [n_axes, T]."""
+        _check(_native.rope_axes_rows(self._h, *self._heads, q, k, positions, axes._addr, q_out, k_out),
+               "vispec_rope_axes_rows")
+
+    def kv_append(self, layer: int, q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor,
+                  positions: Optional[torch.Tensor], axes: Optional[RopeAxes], cu_len: torch.Tensor, kv_len: torch.Tensor,
+                  q_out: Optional[torch.Tensor] = None, kv_len_out: Optional[torch.Tensor] = None) -> None:
+        _check(_native.kv_append(self._h, *self._heads, layer, q, k_new, v_new, positions, axes._addr if axes else 0, cu_len,
+                                 kv_len, q_out, kv_len_out),
+               "vispec_kv_append")
+
+    def kv_append_paged(self, layer: int, q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor,
+                        positions: Optional[torch.Tensor], axes: Optional[RopeAxes], cu_len: torch.Tensor, kv_len: torch.Tensor,
+                        block_table: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                        kv_len_out: Optional[torch.Tensor] = None) -> None:
+        _check(_native.kv_append_paged(self._h, *self._heads, layer, q, k_new, v_new, positions, axes._addr if axes else 0,
+                                       cu_len, kv_len, block_table, q_out, kv_len_out),
+               "vispec_kv_append_paged")
 
     def stream_probe(self, layer: int, kv_len: torch.Tensor, N: int) -> None:
         _check(self.lib.vispec_stream_probe(self.handle, layer, _ptr(kv_len), kv_len.shape[0], N, _stream()),

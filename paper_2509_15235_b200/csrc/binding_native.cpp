@@ -10,9 +10,12 @@
 // the C call.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <climits>
 
 #include "vispec.h"
 
@@ -83,6 +86,59 @@ struct Args {
             return nullptr;
         }
         return static_cast<T*>(t.data_ptr());
+    }
+    // [T, heads, D] bf16 on the current device, a token's heads contiguous, tokens any number of elements apart.  T < 0: the
+    // tensor's own count is taken over, otherwise it has to be T.  None: nullptr.
+    struct Rows { void* p = nullptr; int64_t stride = 0; };
+    Rows rows(int64_t& T, int heads, int D) {
+        Rows r;
+        if (!ok) return r;
+        if (a[i] == Py_None) { ++i; return r; }
+        const at::Tensor* t = tensor(3);
+        if (!t) return r;
+        ++i;
+        if (!t->is_cuda() || t->get_device() != c10::cuda::current_device() || t->scalar_type() != at::kBFloat16) {
+            PyErr_SetString(PyExc_ValueError, "rows must be bfloat16 on the current CUDA device");
+            ok = false;
+        } else if ((T >= 0 && t->size(0) != T) || t->size(1) != heads || t->size(2) != D) {
+            PyErr_Format(PyExc_ValueError, "rows of %lld tokens, %d heads and head size %d are expected", (long long)(T < 0 ? t->size(0) : T), heads, D);
+            ok = false;
+        } else if (t->size(0) > 0 && (t->stride(2) != 1 || (heads > 1 && t->stride(1) != D))) {
+            PyErr_SetString(PyExc_ValueError, "a token's heads must be contiguous");
+            ok = false;
+        }
+        if (!ok) return r;
+        if (t->size(0) > INT_MAX) { PyErr_SetString(PyExc_ValueError, "too many tokens"); ok = false; return r; }
+        T = t->size(0);
+        r.p = t->data_ptr();
+        r.stride = T > 1 ? t->stride(0) : (int64_t)heads * D;      // (one token: whatever its stride says is not used)
+        return r;
+    }
+    // A contiguous int32 tensor on the current device of `n` elements (n < 0: any number).  None: nullptr, where it may be.
+    int32_t* ints(int64_t n, bool optional = false) {
+        if (!ok) return nullptr;
+        PyObject* o = a[i];
+        if (o == Py_None && optional) { ++i; return nullptr; }
+        if (!THPVariable_Check(o)) {
+            PyErr_SetString(PyExc_TypeError, "a CUDA tensor is expected");
+            ok = false;
+            return nullptr;
+        }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || t.scalar_type() != at::kInt || !t.is_contiguous() ||
+            (n >= 0 && t.numel() != n)) {
+            PyErr_Format(PyExc_ValueError, "a contiguous int32 tensor of %lld elements on the current CUDA device is expected", (long long)(n < 0 ? t.numel() : n));
+            ok = false;
+            return nullptr;
+        }
+        ++i;
+        return static_cast<int32_t*>(t.data_ptr());
+    }
+    const vispec_rope_axes* axes() {                                // address of the struct (RopeAxes keeps it), 0: none
+        if (!ok) return nullptr;
+        void* p = PyLong_AsVoidPtr(a[i++]);
+        if (!p && PyErr_Occurred()) ok = false;
+        return static_cast<const vispec_rope_axes*>(p);
     }
 };
 
@@ -307,12 +363,67 @@ NATIVE(tree_rerank) {  // handle, cand_parent, cand_token, cand_score, K, parent
     return finish(g, [&](void* st) { return vispec_tree_rerank(c, cp, ct, cs, B, M, K, parents, ids, sel, st); });
 }
 
+// handle, Hq, Hkv, D, q, k, positions, axes, q_out, k_out
+NATIVE(rope_axes_rows) {
+    Args g(args, nargs, 10);
+    vispec_ctx* c = g.ctx();
+    const int Hq = g.num(), Hkv = g.num(), D = g.num();
+    int64_t T = -1;
+    const auto q = g.rows(T, Hq, D), k = g.rows(T, Hkv, D);
+    if (g.ok && T < 0) { PyErr_SetString(PyExc_TypeError, "q, k or both are tensors"); g.ok = false; }
+    if (g.ok) g.i = 7;                     // the axes say how many positions there are
+    const vispec_rope_axes* axes = g.axes();
+    const auto qo = g.rows(T, Hq, D), ko = g.rows(T, Hkv, D);
+    if (g.ok) g.i = 6;
+    auto* pos = g.ints(axes ? axes->n_axes * T : -1);
+    return finish(g, [&](void* st) { return vispec_rope_axes_rows(c, q.p, q.stride, k.p, k.stride, pos, (int)T, axes, qo.p, qo.stride, ko.p, ko.stride, st); });
+}
+
+// handle, Hq, Hkv, D, layer, q, k_new, v_new, positions, axes, cu_len, kv_len, [block_table,] q_out, kv_len_out
+template <bool PAGED>
+PyObject* kv_append_call(PyObject* const* args, Py_ssize_t nargs) {
+    Args g(args, nargs, PAGED ? 15 : 14);
+    vispec_ctx* c = g.ctx();
+    const int Hq = g.num(), Hkv = g.num(), D = g.num(), layer = g.num();
+    int64_t T = -1;
+    if (g.ok) g.i = 6;
+    const auto k = g.rows(T, Hkv, D), v = g.rows(T, Hkv, D);
+    if (g.ok && (T < 0)) { PyErr_SetString(PyExc_TypeError, "k_new and v_new are tensors"); g.ok = false; }
+    if (g.ok) g.i = 5;
+    const auto q = g.rows(T, Hq, D);
+    if (g.ok) g.i = 9;
+    const vispec_rope_axes* axes = g.axes();
+    if (g.ok) g.i = 8;
+    auto* pos = g.ints(axes ? axes->n_axes * T : -1, true);
+    if (g.ok) g.i = 11;
+    const at::Tensor* tl = g.tensor(1);
+    const int B = tl ? (int)tl->size(0) : 0;
+    if (g.ok) g.i = 10;
+    auto* cu = g.ints(B + 1);
+    auto* kv_len = g.ints(B);
+    int stride = 0;
+    int32_t* table = nullptr;
+    if (PAGED) {
+        const at::Tensor* tt = g.tensor(2);
+        stride = tt ? (int)tt->size(1) : 0;
+        table = g.ints((int64_t)B * stride);
+    }
+    const auto qo = g.rows(T, Hq, D);
+    auto* len_out = g.ints(B, true);
+    return finish(g, [&](void* st) {
+        return PAGED ? vispec_kv_append_paged(c, layer, q.p, q.stride, k.p, k.stride, v.p, v.stride, pos, axes, cu, kv_len, table, stride, B, (int)T, qo.p, qo.stride, len_out, st)
+                     : vispec_kv_append(c, layer, q.p, q.stride, k.p, k.stride, v.p, v.stride, pos, axes, cu, kv_len, B, (int)T, qo.p, qo.stride, len_out, st);
+    });
+}
+NATIVE(kv_append) { return kv_append_call<false>(args, nargs); }
+NATIVE(kv_append_paged) { return kv_append_call<true>(args, nargs); }
+
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     ENTRY(tree_mask_build), ENTRY(tree_verify_attn), ENTRY(tree_verify_attn_rope), ENTRY(tree_verify_attn_paged),
     ENTRY(tree_verify_attn_static), ENTRY(rope_table_build), ENTRY(rope_tree_rows), ENTRY(rope_tree_rows_paged),
     ENTRY(accept), ENTRY(accept_commit), ENTRY(accept_commit_paged), ENTRY(kv_compact), ENTRY(kv_compact_paged),
-    ENTRY(accept_sampled), ENTRY(tree_rerank), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(accept_sampled), ENTRY(tree_rerank), ENTRY(rope_axes_rows), ENTRY(kv_append), ENTRY(kv_append_paged), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Hot calls of libvispec without ctypes", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

@@ -11,13 +11,10 @@
 #include <cuda_bf16.h>
 
 #include "launch.cuh"
+#include "rows.cuh"
 #include "vispec_internal.h"
 
 namespace vispec {
-
-__device__ __forceinline__ void record_status(int* status, int code) {
-    if (status) atomicCAS(status, 0, code);
-}
 
 // ------------------------------------------------------------------------------------------------
 // Ancestor mask (tree of Sec. 3.1 / App. A).  One block per sequence, one thread per node: the
@@ -154,20 +151,6 @@ cudaError_t launch_accept(const int32_t* draft, const int32_t* target, const int
 // already in place and are skipped.
 // ------------------------------------------------------------------------------------------------
 constexpr int kCompactRows = 16;
-
-// Where logical slot `slot` of (sequence b, kv head h) lives, in 16-byte vectors from the tensor's base.
-// Contiguous cache [B,Hkv,S_max,D]: table == nullptr.  Paged pool [num_blocks,Hkv,page_rows,D], or
-// [num_blocks,page_rows,Hkv,D] if token_major: through the block table; -1 if the table entry is outside the pool.
-struct RowMap {
-    const int32_t* table; int table_stride, page_rows, num_blocks, token_major;
-    __device__ __forceinline__ long long at(int b, int h, int slot, int Hkv, int S_max, int chunks) const {
-        if (!table) return (((long long)b * Hkv + h) * S_max + slot) * chunks;
-        const int blk = table[(size_t)b * table_stride + slot / page_rows];
-        if (blk < 0 || blk >= num_blocks) return -1;
-        if (token_major) return (((long long)blk * page_rows + slot % page_rows) * Hkv + h) * chunks;
-        return (((long long)blk * Hkv + h) * page_rows + slot % page_rows) * chunks;
-    }
-};
 
 __global__ void __launch_bounds__(256)
 kv_compact_kernel(void* const* __restrict__ cache_ptrs, int layer_begin, const int32_t* __restrict__ path,

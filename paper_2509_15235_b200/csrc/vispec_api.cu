@@ -1,4 +1,5 @@
 // C ABI of libvispec: context management, argument validation, dispatch to the kernels.
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -492,6 +493,113 @@ int vispec_rope_tree_rows(vispec_ctx* c, int layer, void* q, const void* k_new, 
         return VISPEC_E_CUDA;
     if (B > 0) c->launches += 1;
     return VISPEC_OK;
+}
+
+// The axes' part of the row kernels' arguments; false where the struct does not describe D/2 frequencies.
+static bool set_axes(RowsArgs& a, const vispec_rope_axes* x, int D) {
+    if (x->n_axes < 1 || x->n_axes > VISPEC_MAX_ROPE_AXES || !(x->theta > 1.f) || x->theta > 3.0e38f) return false;
+    int sum = 0;
+    for (int i = 0; i < x->n_axes; ++i) {
+        if (x->sections[i] < 1 || x->sections[i] > D / 2) return false;
+        sum += x->sections[i];
+        a.sections[i] = x->sections[i];
+    }
+    if (sum != D / 2) return false;
+    // dealt in turn: the last turn of axis i > 0 has to lie below D/2 (what is left over then falls to axis 0)
+    for (int i = 1; i < x->n_axes && x->interleaved; ++i)
+        if (x->n_axes * (x->sections[i] - 1) + i >= D / 2) return false;
+    a.n_axes = x->n_axes;
+    a.interleaved = x->interleaved != 0;
+    a.log2_theta = std::log2((double)x->theta);
+    return true;
+}
+static bool row_stride_ok(int64_t stride, int heads, int D) { return stride >= (int64_t)heads * D && stride <= (1ll << 31); }
+
+int vispec_rope_axes_rows(vispec_ctx* c, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const int32_t* positions, int T, const vispec_rope_axes* axes, void* q_out, int64_t q_out_stride,
+                          void* k_out, int64_t k_out_stride, void* stream) {
+    VISPEC_RANGE();
+    if (!c || !axes) return VISPEC_E_NULL;
+    const vispec_shape& s = c->shape;
+    RowsArgs a = {};
+    if (T < 0 || !set_axes(a, axes, s.D)) return VISPEC_E_SHAPE;
+    if (T == 0) return VISPEC_OK;
+    if (!positions || (!q && !k) || !q != !q_out || !k != !k_out) return VISPEC_E_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || (q && ((q_stride | q_out_stride) & 7)) ||
+        (k && ((k_stride | k_out_stride) & 7)))
+        return VISPEC_E_ALIGN;
+    if (q && (!row_stride_ok(q_stride, s.Hq, s.D) || !row_stride_ok(q_out_stride, s.Hq, s.D) || (q == q_out && q_stride != q_out_stride)))
+        return VISPEC_E_SHAPE;
+    if (k && (!row_stride_ok(k_stride, s.Hkv, s.D) || !row_stride_ok(k_out_stride, s.Hkv, s.D) || (k == k_out && k_stride != k_out_stride)))
+        return VISPEC_E_SHAPE;
+    a.q = (const __nv_bfloat16*)q; a.k = (const __nv_bfloat16*)k; a.q_out = (__nv_bfloat16*)q_out; a.k_out = (__nv_bfloat16*)k_out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
+    a.positions = positions; a.T = T; a.Hq = s.Hq; a.Hkv = s.Hkv; a.status = c->d_status;
+    if (launch_prompt_rows(a, false, s.D, c->sm_count, (cudaStream_t)stream) != cudaSuccess) return VISPEC_E_CUDA;
+    c->launches += 1;
+    return VISPEC_OK;
+}
+
+// What the two append calls share; the layer has been looked at.
+static int append_rows(vispec_ctx* c, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                       const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes,
+                       const int32_t* cu_len, const int32_t* kv_len, const int32_t* block_table, int table_stride, int B, int T,
+                       void* q_out, int64_t q_out_stride, int32_t* kv_len_out, void* stream) {
+    const vispec_shape& s = c->shape;
+    RowsArgs a = {};
+    if (axes && !set_axes(a, axes, s.D)) return VISPEC_E_SHAPE;
+    if (B == 0) return VISPEC_OK;
+    if (T > 0) {
+        if (!k_new || !v_new || !q != !q_out || (axes && !positions)) return VISPEC_E_NULL;
+        if (!axes && (q || positions)) return VISPEC_E_SHAPE;
+        if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) || ((k_stride | v_stride) & 7) ||
+            (q && ((q_stride | q_out_stride) & 7)))
+            return VISPEC_E_ALIGN;
+        if (!row_stride_ok(k_stride, s.Hkv, s.D) || !row_stride_ok(v_stride, s.Hkv, s.D)) return VISPEC_E_SHAPE;
+        if (q && (!row_stride_ok(q_stride, s.Hq, s.D) || !row_stride_ok(q_out_stride, s.Hq, s.D) || (q == q_out && q_stride != q_out_stride)))
+            return VISPEC_E_SHAPE;
+    }
+    a.q = (const __nv_bfloat16*)q; a.k = (const __nv_bfloat16*)k_new; a.v = (const __nv_bfloat16*)v_new; a.q_out = (__nv_bfloat16*)q_out;
+    a.k_out = (__nv_bfloat16*)c->h_k[layer]; a.v_out = (__nv_bfloat16*)c->h_v[layer];
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.q_out_stride = q_out_stride;
+    a.positions = positions; a.T = T; a.Hq = s.Hq; a.Hkv = s.Hkv;
+    a.cu_len = cu_len; a.kv_len = kv_len; a.kv_len_out = kv_len_out; a.B = B;
+    const int pr = c->page_rows[layer];
+    a.S_max = pr ? table_stride * pr : s.S_max;
+    a.status = c->d_status;
+    if (launch_prompt_rows(a, true, s.D, c->sm_count, (cudaStream_t)stream, block_table, table_stride, pr, c->num_blocks[layer],
+                           c->token_major[layer]) != cudaSuccess)
+        return VISPEC_E_CUDA;
+    c->launches += 1;
+    return VISPEC_OK;
+}
+
+int vispec_kv_append(vispec_ctx* c, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                     const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes,
+                     const int32_t* cu_len, const int32_t* kv_len, int B, int T, void* q_out, int64_t q_out_stride,
+                     int32_t* kv_len_out, void* stream) {
+    VISPEC_RANGE();
+    if (!c || (B != 0 && (!cu_len || !kv_len))) return VISPEC_E_NULL;
+    if (B < 0 || B > c->shape.B_max || B > kMaxAppendB || T < 0 || (B > 0 && kv_len_out == kv_len)) return VISPEC_E_SHAPE;
+    if (layer < 0 || layer >= c->shape.layers) return VISPEC_E_RANGE;
+    if (!c->h_k[layer]) return VISPEC_E_UNREGISTERED;
+    if (c->page_rows[layer]) return VISPEC_E_UNSUPPORTED;
+    return append_rows(c, layer, q, q_stride, k_new, k_stride, v_new, v_stride, positions, axes, cu_len, kv_len, nullptr, 0, B, T,
+                       q_out, q_out_stride, kv_len_out, stream);
+}
+
+int vispec_kv_append_paged(vispec_ctx* c, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                           const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes,
+                           const int32_t* cu_len, const int32_t* kv_len, const int32_t* block_table, int table_stride, int B, int T,
+                           void* q_out, int64_t q_out_stride, int32_t* kv_len_out, void* stream) {
+    VISPEC_RANGE();
+    if (!c || (B != 0 && (!cu_len || !kv_len || !block_table))) return VISPEC_E_NULL;
+    if (B < 0 || B > c->shape.B_max || B > kMaxAppendB || T < 0 || (B > 0 && kv_len_out == kv_len)) return VISPEC_E_SHAPE;
+    if (layer < 0 || layer >= c->shape.layers) return VISPEC_E_RANGE;
+    const int rc = paged_range_check(c, layer, layer + 1, table_stride);
+    if (rc != VISPEC_OK) return rc;
+    return append_rows(c, layer, q, q_stride, k_new, k_stride, v_new, v_stride, positions, axes, cu_len, kv_len, block_table,
+                       table_stride, B, T, q_out, q_out_stride, kv_len_out, stream);
 }
 
 int vispec_stream_probe(vispec_ctx* c, int layer, const int32_t* kv_len, int B, int N, void* stream) {

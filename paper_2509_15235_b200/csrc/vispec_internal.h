@@ -3,6 +3,7 @@
 
 #include <cuda_runtime.h>
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <stdint.h>
 #include <vector>
 
@@ -67,6 +68,24 @@ cudaError_t launch_rope_rows(void* q, const void* k_new, const void* v_new, cons
                              int num_blocks = 0, int token_major = 0, void* q_out = nullptr, const void* angle_table = nullptr);
 // (q_out: where the rotated q rows go, q itself when null; angle_table: the fp64 half of a vispec_rope_table_build
 // table to take cosines and sines from instead of forming them from positions and theta)
+
+// Rotation of packed rows by several position axes (prompt_rows.cu), with or without their placement in a cache.
+struct RowsArgs {
+    const __nv_bfloat16* q; const __nv_bfloat16* k; const __nv_bfloat16* v;      // [T][heads][D], tokens *_stride elements apart
+    __nv_bfloat16* q_out; __nv_bfloat16* k_out; __nv_bfloat16* v_out;            // (append: k_out, v_out are the caches)
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+    const int32_t* positions;                                                     // [n_axes][T]
+    double log2_theta;
+    int32_t n_axes, sections[VISPEC_MAX_ROPE_AXES], interleaved;                  // n_axes 0: no rotation
+    int T, Hq, Hkv;
+    const int32_t* cu_len; const int32_t* kv_len; int32_t* kv_len_out;            // append only, as B and S_max
+    int B, S_max;
+    int* status;
+};
+constexpr int kMaxAppendB = 8192;              // sequences per append: their ends sit in shared memory
+cudaError_t launch_prompt_rows(const RowsArgs& a, bool append, int D, int sm_count, cudaStream_t st,
+                               const int32_t* block_table = nullptr, int table_stride = 0, int page_rows = 0,
+                               int num_blocks = 0, int token_major = 0);
 
 cudaError_t init_accept_sampled(int device);   // with that device current
 cudaError_t launch_accept_sampled(const int32_t* draft_ids, const int32_t* parents, const float* p, const float* p_hat,
