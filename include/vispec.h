@@ -25,6 +25,7 @@
  *
  *   vispec_rope_axes_rows    rotary embedding of packed q and k rows by several position axes (time, height, width)
  *   vispec_kv_append         a ragged batch of new tokens' k/v rows, rotated on the way, into the cache
+ *   vispec_tree_verify_attn_prefix_paged  the attention of a batch that shares a long prefix, which is read once for all
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless its comment says "host".  The library never takes
@@ -267,6 +268,27 @@ int vispec_cache_register_paged(vispec_ctx* ctx, int layer, void* k_pool, void* 
 int vispec_tree_verify_attn_paged(vispec_ctx* ctx, int layer, const void* q, const int32_t* kv_len,
                                   const int32_t* block_table, int table_stride, const uint64_t* tree_mask, int B, int N,
                                   float scale, void* out, float* lse, void* stream);
+
+/* Attention of a batch whose sequences share a prefix (several samples, questions or drafts behind one image or video, Sec. 5.3's
+ * thousands of image tokens), on a paged layer: the result of vispec_tree_verify_attn_paged (up to the order of its sums) for
+ * sequences whose block tables start with the same blocks, with the prefix read once instead of once per sequence.  N = 1 is
+ * single-token decoding.  Arguments as there, and:
+ *   prefix_len   host: the first prefix_len slots are held by the same blocks for all B sequences, i.e. the first
+ *                floor(prefix_len / page_rows) entries of every row of block_table are those of row 0, the only row whose entries
+ *                are read there.  0: nothing is shared.  Slots of a block that prefix_len ends within are looked up per
+ *                sequence.  Constant in a captured graph.
+ *   scratch      DEVICE, 16-byte aligned, caller-owned, scratch_bytes >= vispec_prefix_scratch_bytes(ctx, B, N): partial results;
+ *                nothing in it has to be cleared or kept.  Calls that may overlap on the GPU need scratch of their own.
+ * kv_len[b] counts the prefix too; a sequence with kv_len[b] below the shared slots or kv_len[b] + N above the table's
+ * capacity gets out = 0, lse = -inf and the status word VISPEC_E_RANGE.  No workspace is used.  At most 128 sequences.
+ * Host errors: E_NULL, E_ALIGN, E_SHAPE, E_RANGE (layer, prefix_len), E_UNREGISTERED, E_UNSUPPORTED (contiguous layer,
+ * B > 128, scale <= 0, sizes beyond 2^31 schedule places), E_WORKSPACE (scratch too small), E_CUDA. */
+int vispec_tree_verify_attn_prefix_paged(vispec_ctx* ctx, int layer, const void* q, const int32_t* kv_len,
+                                         const int32_t* block_table, int table_stride, int prefix_len /*host*/,
+                                         const uint64_t* tree_mask, int B, int N, float scale, void* scratch,
+                                         size_t scratch_bytes, void* out, float* lse, void* stream);
+/* Bytes of scratch for B sequences of N nodes (host call).  Never less for more sequences or nodes. */
+int vispec_prefix_scratch_bytes(const vispec_ctx* ctx, int B, int N, size_t* out /*host*/);
 
 /* vispec_kv_compact on paged layers [layer_begin, layer_end): rows move between logical slots kv_len + path[k]
  * and kv_len + k, each found through block_table (one table serves all layers of the range, which must share

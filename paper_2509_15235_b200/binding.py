@@ -33,6 +33,7 @@ EXPORTS = [
     "vispec_accept_commit_paged", "vispec_rope_tree_rows_paged", "vispec_selftest_bounded_wait",
     "vispec_rope_table_build", "vispec_rope_table_bytes", "vispec_tree_verify_attn_rope",
     "vispec_rope_axes_rows", "vispec_kv_append", "vispec_kv_append_paged",
+    "vispec_prefix_scratch_bytes", "vispec_tree_verify_attn_prefix_paged",
 ]
 OPT_EARLY_PREFETCH = 1
 OPT_FORCE_GENERIC = 2
@@ -115,6 +116,8 @@ def load() -> ctypes.CDLL:
             "vispec_kv_append": [vp, ci, vp, cl, vp, cl, vp, cl, vp, ctypes.POINTER(_RopeAxes), vp, vp, ci, ci, vp, cl, vp, vp],
             "vispec_kv_append_paged": [vp, ci, vp, cl, vp, cl, vp, cl, vp, ctypes.POINTER(_RopeAxes), vp, vp, vp, ci, ci, ci,
                                        vp, cl, vp, vp],
+            "vispec_prefix_scratch_bytes": [vp, ci, ci, ctypes.POINTER(ctypes.c_size_t)],
+            "vispec_tree_verify_attn_prefix_paged": [vp, ci, vp, vp, vp, ci, ci, vp, ci, ci, cf, vp, ctypes.c_size_t, vp, vp, vp],
             "vispec_tree_verify_attn_static": [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp],
         }
         for name, argtypes in sigs.items():
@@ -321,6 +324,19 @@ class VerifyContext:
         _check(_native.kv_append_paged(self._h, *self._heads, layer, q, k_new, v_new, positions, axes._addr if axes else 0,
                                        cu_len, kv_len, block_table, q_out, kv_len_out),
                "vispec_kv_append_paged")
+
+    def prefix_scratch(self, B: int, N: int) -> torch.Tensor:
+        """A scratch tensor for tree_verify_attn_prefix_paged with up to B sequences of N nodes."""
+        n = ctypes.c_size_t()
+        _check(self.lib.vispec_prefix_scratch_bytes(self.handle, B, N, ctypes.byref(n)), "vispec_prefix_scratch_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+
+    def tree_verify_attn_prefix_paged(self, layer: int, q: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor,
+                                      prefix_len: int, tree_mask: torch.Tensor, scale: float, scratch: torch.Tensor,
+                                      out: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
+        _check(_native.tree_verify_attn_prefix_paged(self._h, *self._heads, layer, q, kv_len, block_table, prefix_len,
+                                                     tree_mask, scale, scratch, out, lse),
+               "vispec_tree_verify_attn_prefix_paged")
 
     def stream_probe(self, layer: int, kv_len: torch.Tensor, N: int) -> None:
         _check(self.lib.vispec_stream_probe(self.handle, layer, _ptr(kv_len), kv_len.shape[0], N, _stream()),

@@ -1,0 +1,694 @@
+// Attention of a batch whose sequences share a long prefix (several samples, questions or drafts behind one image or video), on a
+// paged cache whose block tables start with the same blocks: the prefix is read once and scored against the query rows of all
+// sequences together, and each sequence's own keys against its own rows.
+//
+//   For a query row: (m_p, l_p, o_p) over each piece p of its keys, m_p the reference maximum (log2 units), l_p = sum 2^(s - m_p),
+//   o_p = sum 2^(s - m_p) v;   m = max m_p,  l = sum l_p 2^(m_p - m),  out = sum o_p 2^(m_p - m) / l,  lse = (m + log2 l) ln 2.
+//
+// What bounds it: trees of a few sequences make hundreds of rows per kv head, and the prefix costs 4 D flops for each of them a key, so
+// the tensor pipe and the exponentials bound it; with one row per sequence (single-token decoding) it is the read of the keys.
+//
+// Work.  Two kinds of units: (kv head, block of 256 of the batch's B*N*G rows) over the prefix, and (sequence, kv head, block of 256
+// of its N*G rows) over its own keys, both in steps of 128 keys.  All steps lie on one line, the prefix units first, each with its
+// cost (a unit's start costs too), and every CTA, one per SM, takes an equal range of it: no case needs a choice of how many SMs
+// the prefix gets, and the device alone knows kv_len.  A CTA's part of a unit is a segment; each segment parks its rows' (m, l, o)
+// in the scratch, and a second kernel adds up a row's pieces.  (A prefix unit and a sequence's unit always have two pieces to
+// add, so there is nothing to gain from finishing a row in the first kernel.)
+//
+// A segment runs on two accumulator tiles of 128 rows, each with four softmax warps, one thread per row, which work out of phase so that
+// the tensor pipe serves one while the other is in its exponentials, as in attn_tc5_wide.cu:
+//   wide        more than 128 rows: the tiles hold different rows and share every K/V stage
+//   alternate   at most 128 rows: both tiles hold the same rows, tile A takes the even steps and tile B the odd ones, and a row
+//               has two pieces per segment
+// In terms of "operations" j = 0, 1, 2, ... (tile j & 1) the issue order is the same for both: S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ...
+//
+//   warp 0  producer of the K ring (2 x 32 KB)      warp 2  producer of the V ring (3 x 32 KB)
+//   warp 1  issuer of all products                   warp 3  derives the schedule from kv_len
+//   warps 4-7 / 8-11  softmax of tile A / B: thread <-> TMEM lane <-> query row
+// TMEM (512 columns): S_A 0..127, S_B 128..255 (P of the tile, bf16, in the first 64 columns of its S), O_A 256, O_B 384.
+// The waits, time-outs and the programmatic launch are those of attn_tc5.cu.
+#include <cuda_bf16.h>
+
+#include "tc5_common.cuh"
+
+namespace vispec {
+
+using namespace tc5;
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kRows = 256;                     // query rows of a unit
+constexpr uint32_t TMEM_COLS = 512;
+constexpr uint32_t COL_S = 0, COL_O = 256;     // + 128 per tile
+
+enum { X_KFULL = 0, X_KEMPTY = X_KFULL + 2, X_VFULL = X_KEMPTY + 2, X_VEMPTY = X_VFULL + 3, X_SFULL = X_VEMPTY + 3,
+       X_PFULL = X_SFULL + 2 /* [tile][half of the columns] */, X_QFULL = X_PFULL + 4, X_OFULL = X_QFULL + 2, X_OFREE = X_OFULL + 2, X_COUNT = X_OFREE + 2 };
+
+struct PrefixRing {
+    static constexpr int STAGE = 2 * HALF_BYTES, NSK = 2, NSV = 3;
+    static constexpr int OFF_K = 0, OFF_V = NSK * STAGE, OFF_Q = OFF_V + NSV * STAGE;
+    static constexpr int KFULL = X_KFULL, KEMPTY = X_KEMPTY, VFULL = X_VFULL, VEMPTY = X_VEMPTY;
+};
+constexpr int SMEM_BAR = 7 * PrefixRing::STAGE;
+constexpr int BAR_BYTES = 256;
+static_assert(X_COUNT * 8 + 20 <= BAR_BYTES, "barrier block too small");
+constexpr int SMEM_SCHED = SMEM_BAR + BAR_BYTES;
+
+// Where things lie on the line.  Group 0 is the prefix, group b + 1 sequence b.
+struct PrefixSched {
+    int base[kMaxPrefixB + 2];     // where group g starts; base[B + 1] = length of the line
+    int len[kMaxPrefixB];          // sequence b's own committed slots; -1: rejected
+    int range;                     // places of the line per CTA
+};
+constexpr int SMEM_TABRING = SMEM_SCHED + ((int)sizeof(PrefixSched) + 15) / 16 * 16;
+constexpr int SMEM_ALLOC = SMEM_TABRING + 256;
+static_assert(SMEM_ALLOC <= 232448, "over the 227 KB a CTA may have");
+
+struct PrefixParams {
+    const __nv_bfloat16* q; const int32_t* kv_len; const uint64_t* mask;
+    __nv_bfloat16* out; float* lse;
+    // partials: slot s of a region is [D/4][2 half] float4 and [2 half] (m, l); row r of tile x at x * half + r
+    float4* part_o[2]; float2* part_ml[2];     // [0] prefix units, [1] sequences' own
+    int half[2], blocks[2], last_w[2];         // rows per tile in a slot; row blocks per kv head; places of a step of the last one
+    int B, N, Hq, Hkv, G;
+    int P, cap;                                // keys of the prefix; slots a sequence may have beyond it
+    int early, grid;
+    float scale_log2;
+    int* status;
+};
+
+// Places of the line: a wide step, an alternate step, a segment's start.
+constexpr int kWideStep = 16, kAltStep = 12, kSegStart = 32, kMinRange = 48;
+
+__device__ __forceinline__ int unit_places(const PrefixParams& p, int kind, int steps, bool last) {
+    return kSegStart + steps * (last ? p.last_w[kind] : kWideStep);
+}
+__device__ __forceinline__ int head_places(const PrefixParams& p, int kind, int steps) {
+    return steps == 0 ? 0 : (p.blocks[kind] - 1) * unit_places(p, kind, steps, false) + unit_places(p, kind, steps, true);
+}
+__device__ __forceinline__ int own_len(const PrefixParams& p, int kv) {       // -1: rejected
+    return kv >= p.P && kv - p.P <= p.cap - p.N ? kv - p.P : -1;
+}
+__device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
+
+// One warp: exclusive sums of the sequences' places behind the prefix, and the range of a CTA.  store(b, base, len) for each sequence.
+template <typename F>
+__device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const int* kv, F&& store) {
+    int carry = p.Hkv * head_places(p, 0, steps_of(p.P));
+#pragma unroll
+    for (int i = 0; i < kMaxPrefixB / 32; ++i) {
+        if (i * 32 >= p.B) break;
+        const int b = i * 32 + lane;
+        const int S = b < p.B ? own_len(p, kv[i]) : -1;
+        const int len = S >= 0 ? p.Hkv * head_places(p, 1, steps_of(S + p.N)) : 0;
+        int x = len;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        store(i, b, carry + x - len, S);
+        carry += __shfl_sync(0xffffffffu, x, 31);
+    }
+    return carry;
+}
+__device__ __forceinline__ int range_of(int T, int grid) { return max((T + grid - 1) / grid, kMinRange); }
+
+// The first step of a unit that starts at `start` whose place is at or behind g.
+__device__ __forceinline__ int step_at(int g, int start, int w) { const int d = g - start - kSegStart; return d <= 0 ? 0 : (d + w - 1) / w; }
+
+struct PSeg {
+    int b;                    // sequence; 0 for the prefix (its row of the block table is the one that is read)
+    int kind, kvh, st0, n;    // 0 prefix, 1 own keys; kv head; first step and their number
+    int S, total;             // committed keys of the unit, all keys (with the tree's rows)
+    int node0, rows0, rows;   // q row r (of `rows`) of the unit is head (rows0 + r) % G of node node0 + (rows0 + r) / G
+    int slot;
+    bool alt;
+};
+
+struct PIter {
+    const PrefixSched* s; const PrefixParams* p;
+    int g, hi, cta;
+    __device__ __forceinline__ bool next(PSeg& o) {
+        const int B = p->B;
+        for (;;) {
+            if (g >= hi) return false;
+            int l = 0, r = B + 1;                                   // first group with base > g, minus one
+            while (l < r) { const int m = (l + r) >> 1; if (s->base[m] <= g) l = m + 1; else r = m; }
+            const int grp = l - 1, kind = grp > 0 ? 1 : 0;
+            o.kind = kind;
+            o.b = kind ? grp - 1 : 0;
+            o.S = kind ? s->len[o.b] : p->P;
+            o.total = kind ? o.S + p->N : p->P;
+            const int steps = steps_of(o.total), full = unit_places(*p, kind, steps, false), head = head_places(*p, kind, steps);
+            const int rel = g - s->base[grp], nb = p->blocks[kind];
+            o.kvh = rel / head;
+            const int in_head = rel - o.kvh * head, m = min(in_head / full, nb - 1);
+            const int start = s->base[grp] + o.kvh * head + m * full, w = m == nb - 1 ? p->last_w[kind] : kWideStep;
+            o.st0 = step_at(g, start, w);
+            const int end = min(steps, step_at(hi, start, w));
+            o.n = end - o.st0;
+            g = start + kSegStart + steps * w;
+            if (o.n <= 0) continue;
+            o.node0 = kind ? o.b * p->N : 0;
+            o.rows0 = m * kRows;
+            o.rows = min(kRows, (kind ? p->N : p->B * p->N) * p->G - o.rows0);
+            o.alt = o.rows <= 128;
+            o.slot = (kind ? (o.b * p->Hkv + o.kvh) * nb + m : o.kvh * nb + m) + cta;    // units and CTAs both only go up along the line
+            return true;
+        }
+    }
+};
+
+// (pa is not __grid_constant__: the producers hand a changed copy of it on, and with the attribute nvcc 12.9 passed the original)
+__global__ void __launch_bounds__(kThreads, 1)
+attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PrefixParams p,
+                   const PagedArgs pa) {
+    using R = PrefixRing;
+    constexpr int NSK = R::NSK, NSV = R::NSV, STAGE = R::STAGE;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    const uint32_t base = smem_u32(sm);
+    if (base & 1023u) {                        // the swizzled tiles need it; every CTA sees the same base, so all of them leave
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, (int)VISPEC_E_UNSUPPORTED);
+        return;
+    }
+    const uint32_t bars = base + SMEM_BAR;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + SMEM_BAR + X_COUNT * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + SMEM_BAR + X_COUNT * 8 + 8);
+    PrefixSched& sched = *reinterpret_cast<PrefixSched*>(sm + SMEM_SCHED);
+    auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int cta = blockIdx.x;
+
+    if (tid == 0) {
+        for (int i = 0; i < NSK; ++i) { mbar_init(bar(X_KFULL + i), 1); mbar_init(bar(X_KEMPTY + i), 1); }
+        for (int i = 0; i < NSV; ++i) { mbar_init(bar(X_VFULL + i), 1); mbar_init(bar(X_VEMPTY + i), 1); }
+        for (int i = 0; i < 4; ++i) mbar_init(bar(X_PFULL + i), 128);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(X_SFULL + i), 1); mbar_init(bar(X_QFULL + i), 128);
+            mbar_init(bar(X_OFULL + i), 1); mbar_init(bar(X_OFREE + i), 128);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (!p.early) pdl_wait();
+    pdl_launch_dependents();
+    if (warp == 3) {
+        int kv[kMaxPrefixB / 32];
+#pragma unroll
+        for (int i = 0; i < kMaxPrefixB / 32; ++i) kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0;
+        const int T = line_build(p, lane, kv, [&](int, int b, int at, int S) {
+            if (b < p.B) { sched.base[b + 1] = at; sched.len[b] = S; }
+        });
+        if (lane == 0) { sched.base[0] = 0; sched.base[p.B + 1] = T; sched.range = range_of(T, p.grid); }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    auto make_iter = [&]() {
+        const int T = sched.base[p.B + 1], lo = (int)min((long long)cta * sched.range, (long long)T);
+        return PIter{&sched, &p, lo, min(lo + sched.range, T), cta};
+    };
+
+    if (warp == 0 || warp == 2) {
+        // ================= TMA producers: warp 0 the K ring, warp 2 the V ring =================
+        const bool is_v = warp == 2;
+        const uint64_t pol = l2_evict_first_policy();
+        bool waited = !p.early, ok = true;
+        int it = 0;
+        PIter si = make_iter();
+        PSeg sg;
+        const int ns = is_v ? NSV : NSK, full = is_v ? X_VFULL : X_KFULL;
+        while (ok && si.next(sg)) {
+            PagedArgs a = pa;
+            a.N = sg.total - sg.S;
+            if (sg.kind) a.block_table += p.P / pa.page_rows;
+            const uint32_t r = produce_paged<R>(a, &k_map, &v_map, sg.b, sg.kvh, sg.st0, sg.n, sg.S, base, bars,
+                                                base + SMEM_TABRING + (is_v ? 128 : 0), abort_flag, pol, it, waited, lane, is_v ? 2 : 1);
+            it += (int)(r & 0x0fffffffu) + (is_v ? 0 : (int)((r >> 28) & 1u));
+            ok = !((r >> 29) & 1u);
+            waited = (r >> 30) & 1u;
+        }
+        if (*abort_flag && lane == 0) {
+            // drain: wait (bounded, fresh timer) until every copy this warp issued has landed
+            volatile int never = 0;
+            for (int u = max(0, it - ns); u < it; ++u) mbar_wait(bar(full + u % ns), (u / ns) & 1, &never);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ================= issuer of all products (one elected lane; the whole warp walks and waits) =================
+        constexpr uint32_t IDESC_S = instr_desc(0), IDESC_O = instr_desc(1, D);
+        constexpr uint32_t DESC_HI = desc_hi(1024);
+        const bool leader = elect_one();
+        bool ok = true;
+        uint32_t seg = 0;
+        uint32_t sk = 0, pk = 0, sv = 0, pv = 0, pp = 0;   // ring positions with their phases; bit x of pp: phase of tile x's P
+        PIter si = make_iter();
+        PSeg sg;
+        const uint32_t k0 = desc_lo(base + R::OFF_K, 16), v0 = desc_lo(base + R::OFF_V, HALF_BYTES), q0 = desc_lo(base + R::OFF_Q, 16);
+        while (ok && si.next(sg)) {
+            const bool alt = __shfl_sync(0xffffffffu, (int)sg.alt, 0) != 0;
+            const int ops = __shfl_sync(0xffffffffu, sg.alt ? sg.n : 2 * sg.n, 0);
+            auto score = [&](int x) {                      // S_x = Q_x K^T
+                if ((alt || x == 0) && !mbar_wait_warp(bar(X_KFULL) + 8u * sk, pk, abort_flag)) return false;
+                tc_fence_after();
+                const uint32_t kb = k0 + sk * (STAGE >> 4), qb = q0 + x * (STAGE >> 4);
+                const bool done = alt || x == 1;           // nobody else scores this stage
+                if (leader) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
+                        tc_mma_ss(tmem + COL_S + x * 128, qb + off, DESC_HI, kb + off, DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
+                    }
+                    tc_commit(bar(X_SFULL + x));
+                    if (done) tc_commit(bar(X_KEMPTY) + 8u * sk);
+                }
+                if (done && ++sk == NSK) { sk = 0; pk ^= 1; }
+                return true;
+            };
+            for (int x = 0; x < 2 && ok; ++x) {
+                ok = mbar_wait_warp(bar(X_QFULL + x), seg & 1, abort_flag);
+                if (ok && x < ops) ok = score(x);
+            }
+            for (int j = 0; j < ops && ok; ++j) {          // O_x += P_x V(step), half of the tokens as soon as their P is there
+                const int x = j & 1;
+                const uint32_t vb = v0 + sv * (STAGE >> 4);
+                if (alt || x == 0) ok = mbar_wait_warp(bar(X_VFULL) + 8u * sv, pv, abort_flag);
+                // (a segment's first PV product starts a fresh O: the last segment's must have been read)
+                if (ok && j < 2 && seg > 0) ok = mbar_wait_warp(bar(X_OFREE + x), (seg - 1) & 1, abort_flag);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!ok || !(ok = mbar_wait_warp(bar(X_PFULL + 2 * x + h), (pp >> x) & 1, abort_flag))) break;
+                    tc_fence_after();
+                    if (leader) {
+#pragma unroll
+                        for (int ks = h * (STEP / 32); ks < (h + 1) * (STEP / 32); ++ks)
+                            tc_mma_ts(tmem + COL_O + x * 128, tmem + COL_S + x * 128 + ks * 8, vb + ks * 128, DESC_HI, IDESC_O, (j > 1 || ks > 0) ? 1u : 0u);
+                    }
+                }
+                if (!ok) break;
+                pp ^= 1u << x;
+                if (alt || x == 1) {
+                    if (leader) tc_commit(bar(X_VEMPTY) + 8u * sv);
+                    if (++sv == NSV) { sv = 0; pv ^= 1; }
+                }
+                if (j + 2 < ops) ok = score(x);            // overwrites P of this operation, which the product before it reads
+                else if (leader) tc_commit(bar(X_OFULL + x));
+            }
+            // (a tile without an operation waits too: two segments ahead of the issuer its Q barrier would be a phase too far)
+            if (ok && ops == 1 && leader) tc_commit(bar(X_OFULL + 1));
+            ++seg;
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ================= softmax: one thread per query row, tile x by warps 4 + 4x .. 7 + 4x =================
+        const int x = (warp - 4) >> 2, sp = warp & 3;
+        const int tl = sp * 32 + lane;                        // TMEM lane = row of the tile
+        const uint32_t lane_addr = tmem + ((uint32_t)(32 * sp) << 16);
+        const uint32_t s_addr = lane_addr + COL_S + x * 128, o_addr = lane_addr + COL_O + x * 128;
+        pdl_wait();                                           // q, tree_mask and every output come after the preceding kernel
+        const int G = p.G, N = p.N;
+        PIter si = make_iter();
+        PSeg sg;
+        int it = 0, steps_before = 0;                         // operations of this tile so far / steps of all segments so far
+        uint32_t o_phase = 0;
+        bool ok = true;
+        while (ok && si.next(sg)) {
+            const int tile0 = sg.alt ? 0 : x * 128;           // this tile's first row in the unit
+            // Q tile -> shared memory, rows in the swizzled K-major layout of a K stage (every score product of the last
+            // segment has been consumed).  Thread t moves chunk t % QC of rows t / QC, t / QC + QR, ...
+            {
+                constexpr int QC = D / 8, QR = 128 / QC, ITEMS = 128 / QR, BATCH = 8;
+                const int qc = tl % QC;
+#pragma unroll
+                for (int k0 = 0; k0 < ITEMS; k0 += BATCH) {
+                    uint4 v[BATCH];
+#pragma unroll
+                    for (int k = 0; k < BATCH; ++k) {
+                        const int r = tile0 + tl / QC + QR * (k0 + k);
+                        v[k] = make_uint4(0, 0, 0, 0);
+                        if (r < sg.rows) {
+                            const int row = sg.rows0 + r, nd = sg.node0 + row / G, hd = sg.kvh * G + row % G;
+                            v[k] = *(reinterpret_cast<const uint4*>(p.q + ((size_t)nd * p.Hq + hd) * D) + qc);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < BATCH; ++k) {
+                        const int r = tl / QC + QR * (k0 + k);
+                        *reinterpret_cast<uint4*>(sm + R::OFF_Q + x * STAGE + (qc >> 3) * HALF_BYTES + r * 128 + (((qc & 7) ^ (r & 7)) << 4)) = v[k];
+                    }
+                }
+                fence_async_smem();
+                mbar_arrive(bar(X_QFULL + x));
+            }
+            const bool row_ok = tile0 + tl < sg.rows;
+            const bool warp_rows = tile0 + sp * 32 < sg.rows;     // a warp without rows only keeps the barriers going
+            const int S = sg.S, total = sg.total;
+            uint64_t mk0 = 0, mk1 = 0;
+            if (row_ok && sg.kind) {
+                const int W = (N + 63) >> 6;
+                const uint64_t* mrow = p.mask + ((size_t)sg.node0 + (sg.rows0 + tile0 + tl) / G) * W;
+                mk0 = mrow[0];
+                if (W > 1) mk1 = mrow[1];
+                if (N < 64) mk0 &= (1ull << N) - 1;           // bits at or beyond N are not tree nodes
+                if (N < 128) mk1 &= N > 64 ? (1ull << (N - 64)) - 1 : 0ull;
+            }
+            float m_ref = -INFINITY, l_run = 0.f;
+            bool has_o = false;
+
+            for (int t = sg.alt ? x : 0; t < sg.n; t += sg.alt ? 2 : 1, ++it) {
+                const int tok0 = (sg.st0 + t) * STEP;
+                // (this product was issued after the tile's last PV product, so that one is complete too: O and the columns of P are free)
+                if (!mbar_wait_warp(bar(X_SFULL + x), it & 1, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                bool fail = false;
+                if (tok0 + STEP > total) {
+                    // the unit's last step: V rows past the last key may hold anything, and they meet zero weights: made zeros before
+                    // the product (wide: both tiles' warps write them, whichever product comes first)
+                    const int sv = (steps_before + t) % NSV;
+                    fail = !mbar_wait(bar(X_VFULL + sv), ((steps_before + t) / NSV) & 1, abort_flag);
+                    if (!fail && tok0 + tl >= total) {
+                        unsigned char* vrow = sm + R::OFF_V + sv * STAGE + tl * 128;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            *reinterpret_cast<uint4*>(vrow + c * 16) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(vrow + HALF_BYTES + c * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                    }
+                    fence_async_smem();
+                }
+                if (__any_sync(0xffffffffu, fail)) { ok = false; break; }
+                if (!warp_rows) {
+                    tc_fence_before();
+                    mbar_arrive(bar(X_PFULL + 2 * x));
+                    mbar_arrive(bar(X_PFULL + 2 * x + 1));
+                    has_o = true;
+                    continue;
+                }
+                // The row is read from tensor memory in halves of 64 columns, the upper half twice (see attn_tc5_wide.cu).
+                const bool tail = tok0 + STEP > S;                  // reaches past the committed keys: mask bits
+                uint64_t a0 = 0, a1 = 0;                            // bit c of (a0, a1): column c may be attended to
+                if (tail) {
+                    const int t0 = tok0 - S;
+                    if (t0 >= 0) shr128(mk0, mk1, t0, a0, a1); else shl128_fill(mk0, mk1, -t0, a0, a1);
+                }
+                uint32_t s[64];
+                auto load_half = [&](int h) {
+                    tmem_ld32(s_addr + h * 64, s);
+                    tmem_ld32(s_addr + h * 64 + 32, s + 32);
+                    tmem_wait_ld();
+                    if (tail) {
+                        const uint64_t a = h ? a1 : a0;
+#pragma unroll
+                        for (int c = 0; c < 64; ++c)
+                            if (!((a >> c) & 1ull)) s[c] = 0xff800000u;
+                    }
+                };
+                float mx[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mx[e] = -INFINITY;
+#pragma unroll 1
+                for (int h = 1; h >= 0; --h) {
+                    load_half(h);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mx[e] = max3_nan(mx[e], __uint_as_float(s[c + e]), __uint_as_float(s[c + 8 + e]));
+                }
+                const float tmax = max_nan(max3_nan(max3_nan(mx[0], mx[1], mx[2]), max3_nan(mx[3], mx[4], mx[5]), mx[6]), mx[7]) * p.scale_log2;
+                // move the reference maximum only when the tile exceeds it by more than the gap
+                float alpha = 1.f;
+                bool rescale = false;
+                if (tmax > m_ref + kRescaleGap) {         // also true on the first finite tile (m_ref = -inf)
+                    alpha = exp2f(m_ref - tmax);
+                    m_ref = tmax;
+                    l_run *= alpha;
+                    rescale = has_o;
+                }
+                if (!(tmax < INFINITY)) l_run = tmax - tmax;          // a NaN or an infinite score: the row is NaN (see inv_sum)
+                if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t o[16];
+                        tmem_ld16(o_addr + c * 16, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        tmem_st16(o_addr + c * 16, o);
+                    }
+                }
+                const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
+                const uint64_t sc2 = pk2(p.scale_log2, p.scale_log2), mm2 = pk2(-m_use, -m_use);
+                uint64_t sum2 = pk2(0.f, 0.f), sum2b = sum2;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) load_half(1);             // (P of the first half lies in columns 0..31)
+                    uint32_t pd[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        float x0, x1;
+                        up2(fma2(pk2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sc2, mm2), x0, x1);
+                        const float e0 = exp2f(x0), e1 = exp2f(x1);
+                        if (c & 1) sum2b = add2(sum2b, pk2(e0, e1)); else sum2 = add2(sum2, pk2(e0, e1));
+                        pd[c] = pack_bf16(e0, e1);
+                    }
+                    tmem_st32(s_addr + h * 32, pd);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(X_PFULL + 2 * x + h));
+                }
+                float l0, l1;
+                up2(add2(sum2, sum2b), l0, l1);
+                l_run += l0 + l1;
+                has_o = true;
+            }
+            if (!ok) break;
+            steps_before += sg.n;
+
+            // ---- segment epilogue: the row's partial ----
+            if (!(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
+            o_phase ^= 1;
+            tc_fence_after();
+            if (warp_rows) {
+                const int half = p.half[sg.kind];
+                float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * 2 * half + x * half + tl;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(o_addr + c * 32, o);
+                    tmem_wait_ld();
+                    if (row_ok) {
+#pragma unroll
+                        for (int c4 = 0; c4 < 8; ++c4)       // (undefined where no product ran)
+                            prow[(size_t)(c * 8 + c4) * 2 * half] = has_o ? make_float4(__uint_as_float(o[4 * c4]), __uint_as_float(o[4 * c4 + 1]), __uint_as_float(o[4 * c4 + 2]), __uint_as_float(o[4 * c4 + 3]))
+                                                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                }
+                if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * 2 * half + x * half + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
+            }
+            tc_fence_before();
+            mbar_arrive(bar(X_OFREE + x));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(TMEM_COLS) : "memory");
+    }
+    if (tid == 0 && *abort_flag) atomicCAS(p.status, 0, (int)VISPEC_E_TIMEOUT);
+}
+
+// The pieces of a row added up: a thread has C4 groups of four columns of one row; the lanes of a warp have consecutive rows of a
+// (sequence, kv head), which lie side by side in the partials of both kinds.  Four pieces at a time, their loads ahead of the sums.
+template <int C4>
+__global__ void __launch_bounds__(128)
+prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
+    const int lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    const int RG = p.N * p.G, CG = D / 4 / C4;
+    const long long idx = (long long)blockIdx.x * 128 + threadIdx.x, all = (long long)p.B * p.Hkv * RG * CG;
+    const bool live = idx < all;
+    const long long li = live ? idx : all - 1;
+    const int r = (int)(li % RG), cg = (int)(li / RG % CG), kvh = (int)(li / RG / CG % p.Hkv), b = (int)(li / RG / CG / p.Hkv);
+    // the line, from kv_len, which the attention kernel does not write: every lane takes part in the sums, then takes its sequence's
+    int kv[kMaxPrefixB / 32], at[kMaxPrefixB / 32], own[kMaxPrefixB / 32];
+    if (!p.early) pdl_wait();
+#pragma unroll
+    for (int i = 0; i < kMaxPrefixB / 32; ++i) { kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0; at[i] = 0; own[i] = -1; }
+    const int T = line_build(p, lane, kv, [&](int i, int, int place, int S) { at[i] = place; own[i] = S; });
+    int base_b = 0, S = -1;
+#pragma unroll
+    for (int i = 0; i < kMaxPrefixB / 32; ++i) {
+        const int x = __shfl_sync(0xffffffffu, at[i], b & 31), y = __shfl_sync(0xffffffffu, own[i], b & 31);
+        if (b >> 5 == i) { base_b = x; S = y; }
+    }
+    const int R = range_of(T, p.grid);
+    const int node = r / p.G, head = kvh * p.G + r % p.G;
+    // entry e of a kind: piece of CTA c0 + e (wide) or c0 + e / 2, tile e & 1 (alternate)
+    int c0[2], n[2], first[2];
+    bool alt[2];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        const int keys = kind ? S + p.N : p.P, steps = S < 0 ? 0 : steps_of(keys), row = kind ? r : b * RG + r;
+        const int m = row / kRows, lr = row - m * kRows, nb = p.blocks[kind], rows = min(kRows, (kind ? RG : p.B * RG) - m * kRows);
+        n[kind] = 0;
+        if (steps == 0) continue;
+        alt[kind] = rows <= 128;
+        const int w = m == nb - 1 ? p.last_w[kind] : kWideStep;
+        const int u0 = (kind ? base_b : 0) + kvh * head_places(p, kind, steps) + m * unit_places(p, kind, steps, false) + kSegStart;
+        c0[kind] = u0 / R;
+        const int c1 = (u0 + (steps - 1) * w) / R;
+        n[kind] = (c1 - c0[kind] + 1) * (alt[kind] ? 2 : 1);
+        if (steps == 1) n[kind] = 1;                          // (an alternate unit of one step: the second tile has nothing)
+        const int unit = kind ? (b * p.Hkv + kvh) * nb + m : kvh * nb + m;
+        first[kind] = (unit + c0[kind]) * 2 * p.half[kind] + lr % 128 + (!alt[kind] && lr >= 128 ? p.half[kind] : 0);
+    }
+    if (p.early) pdl_wait();
+    if (!live) return;
+    float m_all = -INFINITY, l_all = 0.f;
+    float4 acc[C4];
+#pragma unroll
+    for (int k = 0; k < C4; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int U = C4 == 1 ? 8 : 4;
+    const int entries = n[0] + n[1];
+    for (int e0 = 0; e0 < entries; e0 += U) {
+        float2 ml[U];
+        float4 v[U][C4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = e0 + u;
+            ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int k = 0; k < C4; ++k) v[u][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (e < entries) {
+                const int kind = e < n[0] ? 0 : 1, ek = kind ? e - n[0] : e, half = kind ? p.half[1] : p.half[0];
+                const bool a = kind ? alt[1] : alt[0];
+                const int pos = (kind ? first[1] : first[0]) + (a ? (ek >> 1) * 2 * half + (ek & 1) * half : ek * 2 * half);   // row of the region
+                const int slot = pos / (2 * half), in = pos - slot * 2 * half;
+                ml[u] = __ldcg((kind ? p.part_ml[1] : p.part_ml[0]) + pos);
+                const float4* src = (kind ? p.part_o[1] : p.part_o[0]) + ((size_t)slot * (D / 4) + cg * C4) * 2 * half + in;
+#pragma unroll
+                for (int k = 0; k < C4; ++k) v[u][k] = __ldcg(src + (size_t)k * 2 * half);
+            }
+        }
+        float m_new = m_all;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, ml[u].x);
+        const float m_fin = (m_new == -INFINITY) ? 0.f : m_new;
+        const float a = exp2f(m_all - m_fin);                 // 0 while nothing has been accumulated
+        l_all *= a;
+#pragma unroll
+        for (int k = 0; k < C4; ++k) { acc[k].x *= a; acc[k].y *= a; acc[k].z *= a; acc[k].w *= a; }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float w = exp2f(ml[u].x - m_fin);           // 0 for a piece that saw nothing (or is absent)
+            l_all += ml[u].y * w;
+#pragma unroll
+            for (int k = 0; k < C4; ++k) { acc[k].x += w * v[u][k].x; acc[k].y += w * v[u][k].y; acc[k].z += w * v[u][k].z; acc[k].w += w * v[u][k].w; }
+        }
+        m_all = m_new;
+    }
+    const float inv = inv_sum(l_all);
+    __nv_bfloat16* orow = p.out + (((size_t)b * p.N + node) * p.Hq + head) * D + cg * C4 * 4;
+    if constexpr (C4 == 1) {
+        *reinterpret_cast<uint2*>(orow) = make_uint2(pack_bf16(acc[0].x * inv, acc[0].y * inv), pack_bf16(acc[0].z * inv, acc[0].w * inv));
+    } else {
+#pragma unroll
+        for (int k = 0; k < C4; k += 2)
+            *reinterpret_cast<uint4*>(orow + k * 4) =
+                make_uint4(pack_bf16(acc[k].x * inv, acc[k].y * inv), pack_bf16(acc[k].z * inv, acc[k].w * inv),
+                           pack_bf16(acc[k + 1].x * inv, acc[k + 1].y * inv), pack_bf16(acc[k + 1].z * inv, acc[k + 1].w * inv));
+    }
+    if (p.lse && cg == 0)
+        p.lse[((size_t)b * p.Hq + head) * p.N + node] = l_all > 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+    if (S < 0 && cg == 0 && r == 0 && kvh == 0) atomicCAS(p.status, 0, (int)VISPEC_E_RANGE);
+}
+
+// What of the scratch a call of B sequences of N nodes uses.
+struct PrefixLayout {
+    int rows[2], blocks[2], half[2];
+    long long slots[2];
+    size_t bytes[2];
+};
+PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count) {
+    PrefixLayout l;
+    const int G = Hq / Hkv;
+    for (int kind = 0; kind < 2; ++kind) {
+        l.rows[kind] = (kind ? N : B * N) * G;
+        l.blocks[kind] = (l.rows[kind] + kRows - 1) / kRows;
+        l.half[kind] = l.rows[kind] > 128 ? 128 : (l.rows[kind] + 7) / 8 * 8;
+        l.slots[kind] = (long long)(kind ? B : 1) * Hkv * l.blocks[kind] + sm_count;
+        l.bytes[kind] = (size_t)l.slots[kind] * 2 * l.half[kind] * (D * 4 + 8);
+    }
+    return l;
+}
+
+}  // namespace
+
+size_t prefix_scratch_bytes(int B, int N, int Hq, int Hkv, int sm_count) {
+    const PrefixLayout l = prefix_layout(B, N, Hq, Hkv, sm_count);
+    return l.bytes[0] + l.bytes[1];
+}
+
+cudaError_t init_attn_prefix() {
+    const void* merges[2] = {(const void*)prefix_merge_kernel<1>, (const void*)prefix_merge_kernel<4>};
+    for (const void* m : merges) {                    // (see init_merge)
+        const cudaError_t e = cudaFuncSetAttribute(m, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaFuncSetAttribute((const void*)attn_prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
+}
+
+// Sizes that these kernels take: every place of the line and every row of the partials has a 32-bit number.
+bool attn_prefix_supports(const AttnArgs& a, int prefix) {
+    if (a.B > kMaxPrefixB || !(a.scale > 0.f) || a.D != D || !a.page_rows) return false;
+    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
+    long long T = 0;
+    for (int kind = 0; kind < 2; ++kind) {
+        const long long steps = ((kind ? (long long)a.S_max - prefix : prefix) + STEP - 1) / STEP;
+        T += (kind ? (long long)a.B : 1) * a.Hkv * l.blocks[kind] * (kSegStart + steps * kWideStep);
+        if (l.slots[kind] * 2 * l.half[kind] >= (1ll << 31)) return false;
+    }
+    return T < (1ll << 31) - (1 << 20);
+}
+
+cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cudaStream_t st, int* n_launches) {
+    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
+    PrefixParams p = {};
+    p.q = (const __nv_bfloat16*)a.q; p.kv_len = a.kv_len; p.mask = a.mask;
+    p.out = (__nv_bfloat16*)a.out; p.lse = a.lse;
+    unsigned char* ws = (unsigned char*)scratch;
+    for (int kind = 0; kind < 2; ++kind) {
+        p.part_o[kind] = (float4*)ws;
+        ws += (size_t)l.slots[kind] * 2 * l.half[kind] * D * 4;
+        p.half[kind] = l.half[kind]; p.blocks[kind] = l.blocks[kind];
+        p.last_w[kind] = l.rows[kind] - (l.blocks[kind] - 1) * kRows <= 128 ? kAltStep : kWideStep;
+    }
+    for (int kind = 0; kind < 2; ++kind) { p.part_ml[kind] = (float2*)ws; ws += (size_t)l.slots[kind] * 2 * l.half[kind] * 8; }
+    p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv;
+    p.P = prefix; p.cap = a.S_max - prefix;
+    p.early = a.early_prefetch ? 1 : 0; p.grid = a.sm_count;
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.status = a.status;
+    const PagedArgs pa = {a.block_table, a.table_stride, a.page_rows, a.num_blocks, a.Hkv, a.N, a.token_major, a.status, nullptr};
+    cudaError_t err = launch_pdl(attn_prefix_kernel, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa);
+    if (err != cudaSuccess) return err;
+    ++*n_launches;
+    // One group of four columns per thread while that leaves the SMs with few threads, whole 32-byte sectors of the output beyond.
+    const long long rows = (long long)a.B * a.N * a.Hq;
+    const bool fine = rows * (D / 4) <= 1024ll * a.sm_count;
+    const unsigned blocks = (unsigned)((rows * (fine ? D / 4 : D / 16) + 127) / 128);
+    err = fine ? launch_pdl(prefix_merge_kernel<1>, dim3(blocks), dim3(128), 0, st, 0, p)
+               : launch_pdl(prefix_merge_kernel<4>, dim3(blocks), dim3(128), 0, st, 0, p);
+    if (err == cudaSuccess) ++*n_launches;
+    return err;
+}
+
+}  // namespace vispec

@@ -114,8 +114,8 @@ struct Args {
         r.stride = T > 1 ? t->stride(0) : (int64_t)heads * D;      // (one token: whatever its stride says is not used)
         return r;
     }
-    // A contiguous int32 tensor on the current device of `n` elements (n < 0: any number).  None: nullptr, where it may be.
-    int32_t* ints(int64_t n, bool optional = false) {
+    // A contiguous tensor of `type` and `n` elements on the current device (n < 0: any number).  None: nullptr, where it may be.
+    void* dense(at::ScalarType type, int64_t n, bool optional = false) {
         if (!ok) return nullptr;
         PyObject* o = a[i];
         if (o == Py_None && optional) { ++i; return nullptr; }
@@ -125,15 +125,17 @@ struct Args {
             return nullptr;
         }
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || t.scalar_type() != at::kInt || !t.is_contiguous() ||
+        if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || t.scalar_type() != type || !t.is_contiguous() ||
             (n >= 0 && t.numel() != n)) {
-            PyErr_Format(PyExc_ValueError, "a contiguous int32 tensor of %lld elements on the current CUDA device is expected", (long long)(n < 0 ? t.numel() : n));
+            PyErr_Format(PyExc_ValueError, "a contiguous %s tensor of %lld elements on the current CUDA device is expected",
+                         c10::toString(type), (long long)(n < 0 ? t.numel() : n));
             ok = false;
             return nullptr;
         }
         ++i;
-        return static_cast<int32_t*>(t.data_ptr());
+        return t.data_ptr();
     }
+    int32_t* ints(int64_t n, bool optional = false) { return static_cast<int32_t*>(dense(at::kInt, n, optional)); }
     const vispec_rope_axes* axes() {                                // address of the struct (RopeAxes keeps it), 0: none
         if (!ok) return nullptr;
         void* p = PyLong_AsVoidPtr(a[i++]);
@@ -418,12 +420,36 @@ PyObject* kv_append_call(PyObject* const* args, Py_ssize_t nargs) {
 NATIVE(kv_append) { return kv_append_call<false>(args, nargs); }
 NATIVE(kv_append_paged) { return kv_append_call<true>(args, nargs); }
 
+// handle, Hq, Hkv, D, layer, q, kv_len, block_table, prefix_len, tree_mask, scale, scratch, out, lse
+NATIVE(tree_verify_attn_prefix_paged) {
+    Args g(args, nargs, 14);
+    vispec_ctx* c = g.ctx();
+    const int Hq = g.num(), Hkv = g.num(), D = g.num(), layer = g.num();
+    (void)Hkv;
+    const at::Tensor* t = g.tensor(4);
+    const int64_t B = size(t, 0), N = size(t, 1), all = B * N * Hq;
+    auto* q = g.dense(at::kBFloat16, all * D);
+    auto* kv_len = g.ints(B);
+    const int stride = size(g.tensor(2), 1);
+    auto* table = g.ints(B * stride);
+    const int prefix = g.num();
+    auto* mask = static_cast<uint64_t*>(g.dense(at::kLong, B * N * ((N + 63) / 64)));
+    const float scale = g.real();
+    const at::Tensor* ts = g.tensor(1);
+    auto* scratch = g.dense(at::kByte, -1);
+    const size_t bytes = ts ? (size_t)ts->numel() : 0;
+    auto* out = g.dense(at::kBFloat16, all * D);
+    auto* lse = static_cast<float*>(g.dense(at::kFloat, all, true));
+    return finish(g, [&](void* st) { return vispec_tree_verify_attn_prefix_paged(c, layer, q, kv_len, table, stride, prefix, mask, (int)B, (int)N, scale, scratch, bytes, out, lse, st); });
+}
+
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     ENTRY(tree_mask_build), ENTRY(tree_verify_attn), ENTRY(tree_verify_attn_rope), ENTRY(tree_verify_attn_paged),
     ENTRY(tree_verify_attn_static), ENTRY(rope_table_build), ENTRY(rope_tree_rows), ENTRY(rope_tree_rows_paged),
     ENTRY(accept), ENTRY(accept_commit), ENTRY(accept_commit_paged), ENTRY(kv_compact), ENTRY(kv_compact_paged),
-    ENTRY(accept_sampled), ENTRY(tree_rerank), ENTRY(rope_axes_rows), ENTRY(kv_append), ENTRY(kv_append_paged), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(accept_sampled), ENTRY(tree_rerank), ENTRY(rope_axes_rows), ENTRY(kv_append), ENTRY(kv_append_paged),
+    ENTRY(tree_verify_attn_prefix_paged), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Hot calls of libvispec without ctypes", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

@@ -70,7 +70,8 @@ bool init_device(int device) {
     std::lock_guard<std::mutex> lock(mu);
     if (device < 64 && done[device]) return true;
     const bool ok = init_attn_generic() == cudaSuccess && init_attn_tc5() == cudaSuccess && init_attn_tc5_wide() == cudaSuccess &&
-                    init_stream_probe() == cudaSuccess && init_accept_sampled(device) == cudaSuccess && init_accept_commit() == cudaSuccess;
+                    init_stream_probe() == cudaSuccess && init_accept_sampled(device) == cudaSuccess && init_accept_commit() == cudaSuccess &&
+                    init_attn_prefix() == cudaSuccess;
     if (device < 64) done[device] = ok;
     return ok;
 }
@@ -391,6 +392,48 @@ int vispec_tree_verify_attn_paged(vispec_ctx* c, int layer, const void* q, const
     if (!attn_tc5_supports(a)) return VISPEC_E_UNSUPPORTED;   // B <= 32, scale > 0, workspace large enough for the table's capacity
     int n = 0;
     cudaError_t err = launch_attn_tc5(a, (cudaStream_t)stream, &n);
+    c->launches += n;
+    return err == cudaSuccess ? VISPEC_OK : VISPEC_E_CUDA;
+}
+
+int vispec_prefix_scratch_bytes(const vispec_ctx* c, int B, int N, size_t* out) {
+    if (!c || !out) return VISPEC_E_NULL;
+    if (B < 0 || B > c->shape.B_max || N < 1 || N > c->shape.N_max) return VISPEC_E_SHAPE;
+    *out = B == 0 ? 0 : prefix_scratch_bytes(B, N, c->shape.Hq, c->shape.Hkv, c->sm_count);
+    return VISPEC_OK;
+}
+
+int vispec_tree_verify_attn_prefix_paged(vispec_ctx* c, int layer, const void* q, const int32_t* kv_len,
+                                         const int32_t* block_table, int table_stride, int prefix_len,
+                                         const uint64_t* tree_mask, int B, int N, float scale, void* scratch,
+                                         size_t scratch_bytes, void* out, float* lse, void* stream) {
+    VISPEC_RANGE();
+    if (!c || !q || !kv_len || !block_table || !tree_mask || !out || (!scratch && B > 0)) return VISPEC_E_NULL;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(scratch, 16)) return VISPEC_E_ALIGN;
+    const vispec_shape& s = c->shape;
+    if (B < 0 || B > s.B_max || N < 1 || N > s.N_max || table_stride < 1) return VISPEC_E_SHAPE;
+    if (layer < 0 || layer >= s.layers) return VISPEC_E_RANGE;
+    if (!c->h_k[layer]) return VISPEC_E_UNREGISTERED;
+    const int pr = c->page_rows[layer];
+    if (!pr) return VISPEC_E_UNSUPPORTED;
+    if ((long long)table_stride * pr > (1ll << 30)) return VISPEC_E_SHAPE;
+    if (prefix_len < 0 || prefix_len > table_stride * pr) return VISPEC_E_RANGE;
+    if (B == 0) return VISPEC_OK;
+    AttnArgs a = {};
+    a.q = q; a.k = c->h_k[layer]; a.v = c->h_v[layer];
+    a.kv_len = kv_len; a.mask = tree_mask; a.out = out; a.lse = lse;
+    a.B = B; a.N = N; a.Hq = s.Hq; a.Hkv = s.Hkv; a.D = s.D;
+    a.S_max = table_stride * pr;
+    a.scale = scale; a.status = c->d_status; a.sm_count = c->sm_count;
+    a.early_prefetch = c->early_prefetch;
+    a.k_map = &c->k_map[layer]; a.v_map = &c->v_map[layer];
+    a.block_table = block_table; a.table_stride = table_stride;
+    a.page_rows = pr; a.num_blocks = c->num_blocks[layer]; a.token_major = c->token_major[layer];
+    const int prefix = prefix_len / pr * pr;          // whole blocks: what lies in a started one is each sequence's own
+    if (!attn_prefix_supports(a, prefix)) return VISPEC_E_UNSUPPORTED;
+    if (scratch_bytes < prefix_scratch_bytes(B, N, s.Hq, s.Hkv, c->sm_count)) return VISPEC_E_WORKSPACE;
+    int n = 0;
+    const cudaError_t err = launch_attn_prefix(a, prefix, scratch, (cudaStream_t)stream, &n);
     c->launches += n;
     return err == cudaSuccess ? VISPEC_OK : VISPEC_E_CUDA;
 }

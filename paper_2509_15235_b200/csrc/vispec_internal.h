@@ -134,6 +134,12 @@ struct WidePlan { int ck, grid; double est_us; };   // cluster size (0: even spl
 cudaError_t init_attn_tc5_wide();
 WidePlan attn_tc5_wide_plan(const AttnArgs& a);
 cudaError_t launch_attn_tc5_wide(const AttnArgs& a, const WidePlan& w, cudaStream_t st, int* n_launches);
+// Attention over a prefix that all sequences share, then their own keys (attn_prefix.cu); a.S_max: slots of a table row.
+constexpr int kMaxPrefixB = 128;                  // sequences per call
+size_t prefix_scratch_bytes(int B, int N, int Hq, int Hkv, int sm_count);
+cudaError_t init_attn_prefix();
+bool attn_prefix_supports(const AttnArgs& a, int prefix);
+cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cudaStream_t st, int* n_launches);
 // The bounded wait of the attention kernels on a barrier that never completes (failure-detection self-test).
 cudaError_t launch_bounded_wait_selftest(long long limit, int* status, int* counters, cudaStream_t st);
 // positions[b][i] == kv_len[b] + popcount(mask row i) - 1, else status VISPEC_E_POSITIONS.
