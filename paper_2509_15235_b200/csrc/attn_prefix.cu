@@ -43,7 +43,8 @@ constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;     // + 128 per tile
 
 enum { X_KFULL = 0, X_KEMPTY = X_KFULL + 2, X_VFULL = X_KEMPTY + 2, X_VEMPTY = X_VFULL + 3, X_SFULL = X_VEMPTY + 3,
-       X_PFULL = X_SFULL + 2 /* [tile][half of the columns] */, X_QFULL = X_PFULL + 4, X_OFULL = X_QFULL + 2, X_OFREE = X_OFULL + 2, X_COUNT = X_OFREE + 2 };
+       X_PFULL = X_SFULL + 2 /* [tile][half of the columns] */, X_QWIDE = X_PFULL + 4, X_QALT = X_QWIDE + 2, X_QEMPTY = X_QALT + 2,
+       X_OFULL = X_QEMPTY + 2, X_OFREE = X_OFULL + 2, X_COUNT = X_OFREE + 2 };
 
 struct PrefixRing {
     static constexpr int STAGE = 2 * HALF_BYTES, NSK = 2, NSV = 3;
@@ -186,7 +187,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         for (int i = 0; i < NSV; ++i) { mbar_init(bar(X_VFULL + i), 1); mbar_init(bar(X_VEMPTY + i), 1); }
         for (int i = 0; i < 4; ++i) mbar_init(bar(X_PFULL + i), 128);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(X_SFULL + i), 1); mbar_init(bar(X_QFULL + i), 128);
+            mbar_init(bar(X_SFULL + i), 1);
+            mbar_init(bar(X_QWIDE + i), 129); mbar_init(bar(X_QALT + i), 32); mbar_init(bar(X_QEMPTY + i), 1);
             mbar_init(bar(X_OFULL + i), 1); mbar_init(bar(X_OFREE + i), 128);
         }
         *abort_flag = 0;
@@ -219,7 +221,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     if (warp == 0 || warp == 2) {
         // ================= TMA producers: warp 0 the K ring, warp 2 the V ring =================
         const bool is_v = warp == 2;
-        const uint64_t pol = l2_evict_first_policy();
+        const uint64_t once = l2_evict_first_policy(), again = l2_evict_normal_policy();
         bool waited = !p.early, ok = true;
         int it = 0;
         PIter si = make_iter();
@@ -230,7 +232,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             a.N = sg.total - sg.S;
             if (sg.kind) a.block_table += p.P / pa.page_rows;
             const uint32_t r = produce_paged<R>(a, &k_map, &v_map, sg.b, sg.kvh, sg.st0, sg.n, sg.S, base, bars,
-                                                base + SMEM_TABRING + (is_v ? 128 : 0), abort_flag, pol, it, waited, lane, is_v ? 2 : 1);
+                                                base + SMEM_TABRING + (is_v ? 128 : 0), abort_flag, p.blocks[sg.kind] > 1 ? again : once, it, waited, lane, is_v ? 2 : 1);
             it += (int)(r & 0x0fffffffu) + (is_v ? 0 : (int)((r >> 28) & 1u));
             ok = !((r >> 29) & 1u);
             waited = (r >> 30) & 1u;
@@ -249,16 +251,17 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         bool ok = true;
         uint32_t seg = 0;
         uint32_t sk = 0, pk = 0, sv = 0, pv = 0, pp = 0;   // ring positions with their phases; bit x of pp: phase of tile x's P
+        uint32_t qw = 0, qa = 0, qr = 0;                   // phases of the Q barriers: wide segments, bit r: region r; next region
         PIter si = make_iter();
         PSeg sg;
         const uint32_t k0 = desc_lo(base + R::OFF_K, 16), v0 = desc_lo(base + R::OFF_V, HALF_BYTES), q0 = desc_lo(base + R::OFF_Q, 16);
         while (ok && si.next(sg)) {
             const bool alt = __shfl_sync(0xffffffffu, (int)sg.alt, 0) != 0;
             const int ops = __shfl_sync(0xffffffffu, sg.alt ? sg.n : 2 * sg.n, 0);
-            auto score = [&](int x) {                      // S_x = Q_x K^T
+            auto score = [&](int x, bool last) {           // S_x = Q_x K^T; last: the last one from its Q region
                 if ((alt || x == 0) && !mbar_wait_warp(bar(X_KFULL) + 8u * sk, pk, abort_flag)) return false;
                 tc_fence_after();
-                const uint32_t kb = k0 + sk * (STAGE >> 4), qb = q0 + x * (STAGE >> 4);
+                const uint32_t kb = k0 + sk * (STAGE >> 4), qb = q0 + (alt ? qr : x) * (STAGE >> 4);
                 const bool done = alt || x == 1;           // nobody else scores this stage
                 if (leader) {
 #pragma unroll
@@ -268,13 +271,15 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     }
                     tc_commit(bar(X_SFULL + x));
                     if (done) tc_commit(bar(X_KEMPTY) + 8u * sk);
+                    if (last) tc_commit(bar(X_QEMPTY) + 8u * (alt ? qr : x));
                 }
                 if (done && ++sk == NSK) { sk = 0; pk ^= 1; }
                 return true;
             };
-            for (int x = 0; x < 2 && ok; ++x) {
-                ok = mbar_wait_warp(bar(X_QFULL + x), seg & 1, abort_flag);
-                if (ok && x < ops) ok = score(x);
+            if (alt) ok = mbar_wait_warp(bar(X_QALT) + 8u * qr, (qa >> qr) & 1, abort_flag);
+            for (int x = 0; x < 2 && x < ops && ok; ++x) {
+                if (!alt) ok = mbar_wait_warp(bar(X_QWIDE + x), qw, abort_flag);
+                if (ok) ok = score(x, alt ? x == ops - 1 : ops == 2);
             }
             for (int j = 0; j < ops && ok; ++j) {          // O_x += P_x V(step), half of the tokens as soon as their P is there
                 const int x = j & 1;
@@ -298,14 +303,53 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     if (leader) tc_commit(bar(X_VEMPTY) + 8u * sv);
                     if (++sv == NSV) { sv = 0; pv ^= 1; }
                 }
-                if (j + 2 < ops) ok = score(x);            // overwrites P of this operation, which the product before it reads
+                if (j + 2 < ops) ok = score(x, alt ? j + 3 == ops : j + 4 >= ops);   // overwrites P of this operation, which the product before it reads
                 else if (leader) tc_commit(bar(X_OFULL + x));
             }
-            // (a tile without an operation waits too: two segments ahead of the issuer its Q barrier would be a phase too far)
-            if (ok && ops == 1 && leader) tc_commit(bar(X_OFULL + 1));
+            // (a tile without an operation keeps step as well: neither side may be two phases ahead of the other)
+            if (ok && ops == 1) {
+                if (seg > 0) ok = mbar_wait_warp(bar(X_OFREE + 1), (seg - 1) & 1, abort_flag);
+                if (ok && leader) tc_commit(bar(X_OFULL + 1));
+            }
+            if (alt) { qa ^= 1u << qr; qr ^= 1; } else qw ^= 1;
             ++seg;
         }
         __syncwarp();
+    } else if (warp == 3) {
+        // ================= Q rows of the alternate segments: both tiles score the same rows, so the two Q regions take turns and the
+        // next segment's rows are there before this one has ended (wide segments need both, the softmax threads fill them)
+        pdl_wait();
+        PIter si = make_iter();
+        PSeg sg;
+        int fills[2] = {0, 0}, qr = 0;
+        bool ok = true;
+        while (ok && si.next(sg)) {
+            // (every use of a region is waited for in its turn, also those that the softmax threads fill, and is held up until it has
+            // been: a parity tells only the last two phases apart)
+            if (!sg.alt || qr == 0) ok = mbar_wait_warp(bar(X_QEMPTY), (fills[0]++ & 1) ^ 1, abort_flag);
+            if (ok && (!sg.alt || qr == 1)) ok = mbar_wait_warp(bar(X_QEMPTY + 1), (fills[1]++ & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            if (!sg.alt) {
+                if (lane < 2) mbar_arrive(bar(X_QWIDE + lane));
+                continue;
+            }
+            // half a warp per row, one 16-byte chunk a lane, into the swizzled K-major layout of a K stage.  Rows that do not exist keep
+            // what is there: a row's scores are its own
+            const int c = lane & 15, r0 = lane >> 4;
+            const uint32_t dst = base + R::OFF_Q + qr * STAGE + (c >> 3) * HALF_BYTES;
+            int nd = sg.node0 + (sg.rows0 + r0) / p.G, g = (sg.rows0 + r0) % p.G;
+#pragma unroll 4
+            for (int r = r0; r < sg.rows; r += 2) {
+                const __nv_bfloat16* src = p.q + ((size_t)nd * p.Hq + sg.kvh * p.G + g) * D + c * 8;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "l"(src) : "memory");
+                g += 2;
+                while (g >= p.G) { g -= p.G; ++nd; }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_smem();
+            mbar_arrive(bar(X_QALT) + 8u * qr);
+            qr ^= 1;
+        }
     } else if (warp >= 4) {
         // ================= softmax: one thread per query row, tile x by warps 4 + 4x .. 7 + 4x =================
         const int x = (warp - 4) >> 2, sp = warp & 3;
@@ -318,12 +362,18 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         PSeg sg;
         int it = 0, steps_before = 0;                         // operations of this tile so far / steps of all segments so far
         uint32_t o_phase = 0;
+        int fills[2] = {0, 0}, qr = 0;                        // how often each Q region has been filled; the next alternate segment's
         bool ok = true;
         while (ok && si.next(sg)) {
             const int tile0 = sg.alt ? 0 : x * 128;           // this tile's first row in the unit
-            // Q tile -> shared memory, rows in the swizzled K-major layout of a K stage (every score product of the last
-            // segment has been consumed).  Thread t moves chunk t % QC of rows t / QC, t / QC + QR, ...
-            {
+            // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage.  Thread t moves chunk t % QC of rows
+            // t / QC, t / QC + QR, ...
+            if (sg.alt) {
+                if (qr) ++fills[1]; else ++fills[0];
+                qr ^= 1;
+            } else {
+                if (!(ok = mbar_wait_warp(bar(X_QEMPTY + x), ((x ? fills[1] : fills[0]) & 1) ^ 1, abort_flag))) break;
+                ++fills[0]; ++fills[1];
                 constexpr int QC = D / 8, QR = 128 / QC, ITEMS = 128 / QR, BATCH = 8;
                 const int qc = tl % QC;
 #pragma unroll
@@ -345,7 +395,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     }
                 }
                 fence_async_smem();
-                mbar_arrive(bar(X_QFULL + x));
+                mbar_arrive(bar(X_QWIDE + x));
             }
             const bool row_ok = tile0 + tl < sg.rows;
             const bool warp_rows = tile0 + sp * 32 < sg.rows;     // a warp without rows only keeps the barriers going
