@@ -117,7 +117,10 @@ __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const
 __device__ __forceinline__ int range_of(int T, int grid) { return max((T + grid - 1) / grid, kMinRange); }
 
 // The first step of a unit that starts at `start` whose place is at or behind g.
-__device__ __forceinline__ int step_at(int g, int start, int w) { const int d = g - start - kSegStart; return d <= 0 ? 0 : (d + w - 1) / w; }
+__device__ __forceinline__ int step_at(int g, int start, bool wide) {
+    const int d = g - start - kSegStart;
+    return d <= 0 ? 0 : wide ? (d + kWideStep - 1) / kWideStep : (d + kAltStep - 1) / kAltStep;
+}
 
 struct PSeg {
     int b;                    // sequence; 0 for the prefix (its row of the block table is the one that is read)
@@ -128,39 +131,58 @@ struct PSeg {
     bool alt;
 };
 
+// A CTA's segments, in their order.  Only the first unit is looked up; from one unit to the next it goes by counting (a lookup's
+// divisions and dependent loads took every role 1500 cycles a segment, a sixth of a short segment).
 struct PIter {
     const PrefixSched* s; const PrefixParams* p;
-    int g, hi, cta;
+    int lo, hi, cta;
+    int grp, kvh, m, start;      // the unit that comes next: group, kv head, row block, where it starts
+    __device__ __forceinline__ PIter(const PrefixSched* s_, const PrefixParams* p_, int lo_, int hi_, int cta_)
+        : s(s_), p(p_), lo(lo_), hi(hi_), cta(cta_), grp(0), kvh(0), m(0), start(hi_) {
+        if (lo >= hi) return;
+        int l = 0, r = p->B + 1;                                    // first group with base > lo, minus one
+        while (l < r) { const int x = (l + r) >> 1; if (s->base[x] <= lo) l = x + 1; else r = x; }
+        grp = l - 1;
+        const int kind = grp > 0 ? 1 : 0, steps = steps_of(keys(kind)), full = unit_places(*p, kind, steps, false), head = head_places(*p, kind, steps);
+        const int rel = lo - s->base[grp];
+        kvh = rel / head;
+        m = min((rel - kvh * head) / full, p->blocks[kind] - 1);
+        start = s->base[grp] + kvh * head + m * full;
+    }
+    __device__ __forceinline__ int keys(int kind) const { return kind ? s->len[grp - 1] + p->N : p->P; }
     __device__ __forceinline__ bool next(PSeg& o) {
-        const int B = p->B;
-        for (;;) {
-            if (g >= hi) return false;
-            int l = 0, r = B + 1;                                   // first group with base > g, minus one
-            while (l < r) { const int m = (l + r) >> 1; if (s->base[m] <= g) l = m + 1; else r = m; }
-            const int grp = l - 1, kind = grp > 0 ? 1 : 0;
+        while (start < hi) {
+            const int kind = grp > 0 ? 1 : 0, nb = p->blocks[kind];
             o.kind = kind;
             o.b = kind ? grp - 1 : 0;
-            o.S = kind ? s->len[o.b] : p->P;
-            o.total = kind ? o.S + p->N : p->P;
-            const int steps = steps_of(o.total), full = unit_places(*p, kind, steps, false), head = head_places(*p, kind, steps);
-            const int rel = g - s->base[grp], nb = p->blocks[kind];
-            o.kvh = rel / head;
-            const int in_head = rel - o.kvh * head, m = min(in_head / full, nb - 1);
-            const int start = s->base[grp] + o.kvh * head + m * full, w = m == nb - 1 ? p->last_w[kind] : kWideStep;
-            o.st0 = step_at(g, start, w);
-            const int end = min(steps, step_at(hi, start, w));
-            o.n = end - o.st0;
-            g = start + kSegStart + steps * w;
-            if (o.n <= 0) continue;
-            o.node0 = kind ? o.b * p->N : 0;
+            o.total = keys(kind);
+            o.S = kind ? o.total - p->N : o.total;
+            o.kvh = kvh;
             o.rows0 = m * kRows;
             o.rows = min(kRows, (kind ? p->N : p->B * p->N) * p->G - o.rows0);
             o.alt = o.rows <= 128;
-            o.slot = (kind ? (o.b * p->Hkv + o.kvh) * nb + m : o.kvh * nb + m) + cta;    // units and CTAs both only go up along the line
-            return true;
+            o.node0 = o.b * p->N;
+            o.slot = (o.b * p->Hkv + kvh) * nb + m + cta;           // units and CTAs both only go up along the line
+            const int steps = steps_of(o.total), here = start;
+            start += kSegStart + steps * (o.alt ? kAltStep : kWideStep);
+            o.st0 = step_at(lo, here, !o.alt);
+            o.n = min(steps, step_at(hi, here, !o.alt)) - o.st0;
+            if (++m == nb) {
+                m = 0;
+                if (++kvh == p->Hkv) {
+                    kvh = 0;
+                    do ++grp; while (grp <= p->B && s->base[grp + 1] == start);     // groups without units
+                }
+            }
+            if (o.n > 0) return true;
         }
+        return false;
     }
 };
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
 // (pa is not __grid_constant__: the producers hand a changed copy of it on, and with the attribute nvcc 12.9 passed the original)
 __global__ void __launch_bounds__(kThreads, 1)
@@ -215,7 +237,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     const uint32_t tmem = *tmem_slot;
     auto make_iter = [&]() {
         const int T = sched.base[p.B + 1], lo = (int)min((long long)cta * sched.range, (long long)T);
-        return PIter{&sched, &p, lo, min(lo + sched.range, T), cta};
+        return PIter(&sched, &p, lo, min(lo + sched.range, T), cta);
     };
 
     if (warp == 0 || warp == 2) {
@@ -340,8 +362,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             int nd = sg.node0 + (sg.rows0 + r0) / p.G, g = (sg.rows0 + r0) % p.G;
 #pragma unroll 4
             for (int r = r0; r < sg.rows; r += 2) {
-                const __nv_bfloat16* src = p.q + ((size_t)nd * p.Hq + sg.kvh * p.G + g) * D + c * 8;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "l"(src) : "memory");
+                cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + ((size_t)nd * p.Hq + sg.kvh * p.G + g) * D + c * 8);
                 g += 2;
                 while (g >= p.G) { g -= p.G; ++nd; }
             }
@@ -366,34 +387,25 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         bool ok = true;
         while (ok && si.next(sg)) {
             const int tile0 = sg.alt ? 0 : x * 128;           // this tile's first row in the unit
-            // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage.  Thread t moves chunk t % QC of rows
-            // t / QC, t / QC + QR, ...
+            // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage.  Thread t moves chunk t % 16 of rows
+            // t / 16, t / 16 + 8, ... (a loop of little code: unrolled with its divisions it took 8000 cycles, most of them the fetch of its code)
             if (sg.alt) {
                 if (qr) ++fills[1]; else ++fills[0];
                 qr ^= 1;
             } else {
                 if (!(ok = mbar_wait_warp(bar(X_QEMPTY + x), ((x ? fills[1] : fills[0]) & 1) ^ 1, abort_flag))) break;
                 ++fills[0]; ++fills[1];
-                constexpr int QC = D / 8, QR = 128 / QC, ITEMS = 128 / QR, BATCH = 8;
-                const int qc = tl % QC;
-#pragma unroll
-                for (int k0 = 0; k0 < ITEMS; k0 += BATCH) {
-                    uint4 v[BATCH];
-#pragma unroll
-                    for (int k = 0; k < BATCH; ++k) {
-                        const int r = tile0 + tl / QC + QR * (k0 + k);
-                        v[k] = make_uint4(0, 0, 0, 0);
-                        if (r < sg.rows) {
-                            const int row = sg.rows0 + r, nd = sg.node0 + row / G, hd = sg.kvh * G + row % G;
-                            v[k] = *(reinterpret_cast<const uint4*>(p.q + ((size_t)nd * p.Hq + hd) * D) + qc);
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < BATCH; ++k) {
-                        const int r = tl / QC + QR * (k0 + k);
-                        *reinterpret_cast<uint4*>(sm + R::OFF_Q + x * STAGE + (qc >> 3) * HALF_BYTES + r * 128 + (((qc & 7) ^ (r & 7)) << 4)) = v[k];
-                    }
+                const int c = tl & 15, step_nd = 8 / G, step_g = 8 % G;
+                const uint32_t dst = base + R::OFF_Q + x * STAGE + (c >> 3) * HALF_BYTES;
+                int nd = sg.node0 + (sg.rows0 + tile0 + (tl >> 4)) / G, g = (sg.rows0 + tile0 + (tl >> 4)) % G;
+#pragma unroll 2
+                for (int r = tl >> 4; r < min(128, sg.rows - tile0); r += 8) {     // (rows that do not exist keep what is there)
+                    cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + ((size_t)nd * p.Hq + sg.kvh * G + g) * D + c * 8);
+                    nd += step_nd;
+                    g += step_g;
+                    if (g >= G) { g -= G; ++nd; }
                 }
+                asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_async_smem();
                 mbar_arrive(bar(X_QWIDE + x));
             }
@@ -525,25 +537,27 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             if (!(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
             o_phase ^= 1;
             tc_fence_after();
+            // O is free for the next segment's products as soon as it has been read, ahead of the last stores.  (No partial is read before
+            // this kernel has ended, so the arrival need not wait for them.)
             if (warp_rows) {
-                const int half = p.half[sg.kind];
-                float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * 2 * half + x * half + tl;
+                const int rows2 = 2 * p.half[sg.kind];
+                float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * rows2 + x * (rows2 >> 1) + tl;
+                if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * rows2 + x * (rows2 >> 1) + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
                     tmem_ld32(o_addr + c * 32, o);
                     tmem_wait_ld();
-                    if (row_ok) {
+                    if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
+                    if (row_ok && has_o) {                    // (without a product the piece has l = 0 and its o is not looked at)
 #pragma unroll
-                        for (int c4 = 0; c4 < 8; ++c4)       // (undefined where no product ran)
-                            prow[(size_t)(c * 8 + c4) * 2 * half] = has_o ? make_float4(__uint_as_float(o[4 * c4]), __uint_as_float(o[4 * c4 + 1]), __uint_as_float(o[4 * c4 + 2]), __uint_as_float(o[4 * c4 + 3]))
-                                                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int c4 = 0; c4 < 8; ++c4, prow += rows2)
+                            *prow = make_float4(__uint_as_float(o[4 * c4]), __uint_as_float(o[4 * c4 + 1]), __uint_as_float(o[4 * c4 + 2]), __uint_as_float(o[4 * c4 + 3]));
                     }
                 }
-                if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * 2 * half + x * half + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
+            } else {
+                mbar_arrive(bar(X_OFREE + x));
             }
-            tc_fence_before();
-            mbar_arrive(bar(X_OFREE + x));
         }
     }
     tc_fence_before();
@@ -640,6 +654,7 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
         for (int u = 0; u < U; ++u) {
             const float w = exp2f(ml[u].x - m_fin);           // 0 for a piece that saw nothing (or is absent)
             l_all += ml[u].y * w;
+            if (ml[u].x == -INFINITY) continue;               // (its o may never have been written)
 #pragma unroll
             for (int k = 0; k < C4; ++k) { acc[k].x += w * v[u][k].x; acc[k].y += w * v[u][k].y; acc[k].z += w * v[u][k].z; acc[k].w += w * v[u][k].w; }
         }
