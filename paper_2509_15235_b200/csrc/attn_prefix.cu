@@ -18,9 +18,9 @@
 // A segment runs on two accumulator tiles of 128 rows, each with four softmax warps, one thread per row, which work out of phase so that
 // the tensor pipe serves one while the other is in its exponentials, as in attn_tc5_wide.cu:
 //   wide        more than 128 rows: the tiles hold different rows and share every K/V stage
-//   alternate   at most 128 rows: both tiles hold the same rows, tile A takes the even steps and tile B the odd ones, and a row
-//               has two pieces per segment
-// In terms of "operations" j = 0, 1, 2, ... (tile j & 1) the issue order is the same for both: S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ...
+//   alternate   at most 128 rows: both tiles hold the same rows and take turns at the steps, and a row has two pieces per segment
+// In terms of "operations" 0, 1, 2, ... (one tile's share of a step; the tiles take turns, across segments too) the issue order is
+// always S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ...
 //
 //   warp 0  producer of the K ring (2 x 32 KB)      warp 2  producer of the V ring (3 x 32 KB)
 //   warp 1  issuer of all products                   warp 3  derives the schedule from kv_len
@@ -71,19 +71,24 @@ struct PrefixParams {
     __nv_bfloat16* out; float* lse;
     // partials: slot s of a region is [D/4][2 half] float4 and [2 half] (m, l); row r of tile x at x * half + r
     float4* part_o[2]; float2* part_ml[2];     // [0] prefix units, [1] sequences' own
-    int half[2], blocks[2], last_w[2];         // rows per tile in a slot; row blocks per kv head; places of a step of the last one
+    int half[2], blocks[2], last_alt[2];       // rows per tile in a slot; row blocks per kv head; is the last one alternate?
     int B, N, Hq, Hkv, G;
     int P, cap;                                // keys of the prefix; slots a sequence may have beyond it
     int early, grid;
+    int groups;                                // sequences whose own keys are on the line: B, or 0 where few_rows_kernel takes them
     float scale_log2;
     int* status;
 };
 
-// Places of the line: a wide step, an alternate step, a segment's start.
-constexpr int kWideStep = 16, kAltStep = 12, kSegStart = 32, kMinRange = 48;
+// Places of the line (some 210 cycles each, from clock stamps of 8 x 60 nodes of 32/32 heads): a wide step 3400 cycles, an alternate
+// one 1900, the start of a segment (Q rows, first score, last product, partials) 7500 and 3500.
+constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 48;
+__host__ __device__ constexpr int step_places(bool alt) { return alt ? kAltStep : kWideStep; }
+__host__ __device__ constexpr int start_places(bool alt) { return alt ? kAltStart : kWideStart; }
 
 __device__ __forceinline__ int unit_places(const PrefixParams& p, int kind, int steps, bool last) {
-    return kSegStart + steps * (last ? p.last_w[kind] : kWideStep);
+    const bool alt = last && p.last_alt[kind];
+    return start_places(alt) + steps * step_places(alt);
 }
 __device__ __forceinline__ int head_places(const PrefixParams& p, int kind, int steps) {
     return steps == 0 ? 0 : (p.blocks[kind] - 1) * unit_places(p, kind, steps, false) + unit_places(p, kind, steps, true);
@@ -99,9 +104,9 @@ __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const
     int carry = p.Hkv * head_places(p, 0, steps_of(p.P));
 #pragma unroll
     for (int i = 0; i < kMaxPrefixB / 32; ++i) {
-        if (i * 32 >= p.B) break;
+        if (i * 32 >= p.groups) break;
         const int b = i * 32 + lane;
-        const int S = b < p.B ? own_len(p, kv[i]) : -1;
+        const int S = b < p.groups ? own_len(p, kv[i]) : -1;
         const int len = S >= 0 ? p.Hkv * head_places(p, 1, steps_of(S + p.N)) : 0;
         int x = len;
 #pragma unroll
@@ -117,9 +122,9 @@ __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const
 __device__ __forceinline__ int range_of(int T, int grid) { return max((T + grid - 1) / grid, kMinRange); }
 
 // The first step of a unit that starts at `start` whose place is at or behind g.
-__device__ __forceinline__ int step_at(int g, int start, bool wide) {
-    const int d = g - start - kSegStart;
-    return d <= 0 ? 0 : wide ? (d + kWideStep - 1) / kWideStep : (d + kAltStep - 1) / kAltStep;
+__device__ __forceinline__ int step_at(int g, int start, bool alt) {
+    const int d = g - start - start_places(alt);
+    return d <= 0 ? 0 : alt ? (d + kAltStep - 1) / kAltStep : (d + kWideStep - 1) / kWideStep;
 }
 
 struct PSeg {
@@ -136,42 +141,51 @@ struct PSeg {
 struct PIter {
     const PrefixSched* s; const PrefixParams* p;
     int lo, hi, cta;
-    int grp, kvh, m, start;      // the unit that comes next: group, kv head, row block, where it starts
+    int grp, kvh, m, start;                  // the unit that comes next: group, kv head, row block, where it starts
+    int kind, steps, full, last;             // its group: prefix or own, steps of a unit, places of one with 256 rows, of a head's last one
+    __device__ __forceinline__ void enter() {
+        kind = grp > 0 ? 1 : 0;
+        steps = steps_of(kind ? s->len[grp - 1] + p->N : p->P);
+        full = unit_places(*p, kind, steps, false);
+        last = unit_places(*p, kind, steps, true);
+    }
     __device__ __forceinline__ PIter(const PrefixSched* s_, const PrefixParams* p_, int lo_, int hi_, int cta_)
         : s(s_), p(p_), lo(lo_), hi(hi_), cta(cta_), grp(0), kvh(0), m(0), start(hi_) {
         if (lo >= hi) return;
-        int l = 0, r = p->B + 1;                                    // first group with base > lo, minus one
+        int l = 0, r = p->groups + 1;                                    // first group with base > lo, minus one
         while (l < r) { const int x = (l + r) >> 1; if (s->base[x] <= lo) l = x + 1; else r = x; }
         grp = l - 1;
-        const int kind = grp > 0 ? 1 : 0, steps = steps_of(keys(kind)), full = unit_places(*p, kind, steps, false), head = head_places(*p, kind, steps);
-        const int rel = lo - s->base[grp];
+        enter();
+        const int rel = lo - s->base[grp], head = (p->blocks[kind] - 1) * full + last;
         kvh = rel / head;
         m = min((rel - kvh * head) / full, p->blocks[kind] - 1);
         start = s->base[grp] + kvh * head + m * full;
     }
-    __device__ __forceinline__ int keys(int kind) const { return kind ? s->len[grp - 1] + p->N : p->P; }
     __device__ __forceinline__ bool next(PSeg& o) {
         while (start < hi) {
-            const int kind = grp > 0 ? 1 : 0, nb = p->blocks[kind];
+            const int nb = p->blocks[kind], here = start;
             o.kind = kind;
             o.b = kind ? grp - 1 : 0;
-            o.total = keys(kind);
-            o.S = kind ? o.total - p->N : o.total;
+            o.S = kind ? s->len[grp - 1] : p->P;
+            o.total = kind ? o.S + p->N : o.S;
             o.kvh = kvh;
             o.rows0 = m * kRows;
             o.rows = min(kRows, (kind ? p->N : p->B * p->N) * p->G - o.rows0);
             o.alt = o.rows <= 128;
             o.node0 = o.b * p->N;
             o.slot = (o.b * p->Hkv + kvh) * nb + m + cta;           // units and CTAs both only go up along the line
-            const int steps = steps_of(o.total), here = start;
-            start += kSegStart + steps * (o.alt ? kAltStep : kWideStep);
-            o.st0 = step_at(lo, here, !o.alt);
-            o.n = min(steps, step_at(hi, here, !o.alt)) - o.st0;
+            o.st0 = 0;
+            o.n = steps;
+            start += m == nb - 1 ? last : full;
+            if (here < lo) o.st0 = step_at(lo, here, o.alt);
+            if (start > hi) o.n = step_at(hi, here, o.alt);        // (at most the unit's steps)
+            o.n -= o.st0;
             if (++m == nb) {
                 m = 0;
                 if (++kvh == p->Hkv) {
                     kvh = 0;
-                    do ++grp; while (grp <= p->B && s->base[grp + 1] == start);     // groups without units
+                    do ++grp; while (grp <= p->groups && s->base[grp + 1] == start);     // groups without units
+                    if (start < hi) enter();
                 }
             }
             if (o.n > 0) return true;
@@ -221,22 +235,21 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (!p.early) pdl_wait();
-    pdl_launch_dependents();
     if (warp == 3) {
         int kv[kMaxPrefixB / 32];
 #pragma unroll
         for (int i = 0; i < kMaxPrefixB / 32; ++i) kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0;
         const int T = line_build(p, lane, kv, [&](int, int b, int at, int S) {
-            if (b < p.B) { sched.base[b + 1] = at; sched.len[b] = S; }
+            if (b < p.groups) { sched.base[b + 1] = at; sched.len[b] = S; }
         });
-        if (lane == 0) { sched.base[0] = 0; sched.base[p.B + 1] = T; sched.range = range_of(T, p.grid); }
+        if (lane == 0) { sched.base[0] = 0; sched.base[p.groups + 1] = T; sched.range = range_of(T, p.grid); }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     auto make_iter = [&]() {
-        const int T = sched.base[p.B + 1], lo = (int)min((long long)cta * sched.range, (long long)T);
+        const int T = sched.base[p.groups + 1], lo = (int)min((long long)cta * sched.range, (long long)T);
         return PIter(&sched, &p, lo, min(lo + sched.range, T), cta);
     };
 
@@ -270,71 +283,115 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         constexpr uint32_t IDESC_S = instr_desc(0), IDESC_O = instr_desc(1, D);
         constexpr uint32_t DESC_HI = desc_hi(1024);
         const bool leader = elect_one();
-        bool ok = true;
-        uint32_t seg = 0;
-        uint32_t sk = 0, pk = 0, sv = 0, pv = 0, pp = 0;   // ring positions with their phases; bit x of pp: phase of tile x's P
-        uint32_t qw = 0, qa = 0, qr = 0;                   // phases of the Q barriers: wide segments, bit r: region r; next region
+        const uint32_t k0 = desc_lo(base + R::OFF_K, 16), v0 = desc_lo(base + R::OFF_V, HALF_BYTES), q0 = desc_lo(base + R::OFF_Q, 16);
         PIter si = make_iter();
         PSeg sg;
-        const uint32_t k0 = desc_lo(base + R::OFF_K, 16), v0 = desc_lo(base + R::OFF_V, HALF_BYTES), q0 = desc_lo(base + R::OFF_Q, 16);
-        while (ok && si.next(sg)) {
-            const bool alt = __shfl_sync(0xffffffffu, (int)sg.alt, 0) != 0;
-            const int ops = __shfl_sync(0xffffffffu, sg.alt ? sg.n : 2 * sg.n, 0);
-            auto score = [&](int x, bool last) {           // S_x = Q_x K^T; last: the last one from its Q region
-                if ((alt || x == 0) && !mbar_wait_warp(bar(X_KFULL) + 8u * sk, pk, abort_flag)) return false;
+        uint32_t sk = 0, pk = 0, sv = 0, pv = 0, pp = 0;   // ring positions with their phases; bit x of pp: phase of tile x's P
+        uint32_t qw = 0, qa = 0, qr = 0;                   // phases of the Q barriers: wide segments, bit r: region r; next region
+        int sx = 0, px = 0, seg = 0;                       // alternate segments: tiles of the next score and PV product
+        bool ok = true;
+        // this segment and the one behind it: 0 steps where there is none
+        auto fetch = [&](int& n, bool& alt) {
+            const bool live = si.next(sg);
+            alt = __shfl_sync(0xffffffffu, (int)sg.alt, 0) != 0;
+            n = live ? __shfl_sync(0xffffffffu, sg.n, 0) : 0;
+        };
+        auto wait = [&](int i, uint32_t parity) { return ok = mbar_wait_warp(bar(i), parity, abort_flag); };
+        // S_x = Q K^T of the K stage sk, Q from region r
+        auto score = [&](int x, uint32_t r, bool stage_done, bool q_done) {
+            tc_fence_after();
+            if (leader) {
+                const uint32_t kb = k0 + sk * (STAGE >> 4), qb = q0 + r * (STAGE >> 4);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
+                    tc_mma_ss(tmem + COL_S + x * 128, qb + off, DESC_HI, kb + off, DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
+                }
+                tc_commit(bar(X_SFULL + x));
+                if (stage_done) tc_commit(bar(X_KEMPTY) + 8u * sk);
+                if (q_done) tc_commit(bar(X_QEMPTY) + 8u * r);                     // the last score from this Q region
+            }
+            if (stage_done && ++sk == NSK) { sk = 0; pk ^= 1; }
+        };
+        // O_x (+)= P_x V of the V stage sv, half of the tokens as soon as their P is there
+        auto product = [&](int x, bool fresh, bool stage_done) {
+            const uint32_t vb = v0 + sv * (STAGE >> 4);
+            // (a segment's first PV product starts a fresh O: the last segment's must have been read)
+            if (fresh && seg > 0 && !wait(X_OFREE + x, (seg - 1) & 1)) return;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!wait(X_PFULL + 2 * x + h, (pp >> x) & 1)) return;
                 tc_fence_after();
-                const uint32_t kb = k0 + sk * (STAGE >> 4), qb = q0 + (alt ? qr : x) * (STAGE >> 4);
-                const bool done = alt || x == 1;           // nobody else scores this stage
                 if (leader) {
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
-                        tc_mma_ss(tmem + COL_S + x * 128, qb + off, DESC_HI, kb + off, DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
-                    }
-                    tc_commit(bar(X_SFULL + x));
-                    if (done) tc_commit(bar(X_KEMPTY) + 8u * sk);
-                    if (last) tc_commit(bar(X_QEMPTY) + 8u * (alt ? qr : x));
+                    for (int ks = h * (STEP / 32); ks < (h + 1) * (STEP / 32); ++ks)
+                        tc_mma_ts(tmem + COL_O + x * 128, tmem + COL_S + x * 128 + ks * 8, vb + ks * 128, DESC_HI, IDESC_O, (!fresh || ks > 0) ? 1u : 0u);
                 }
-                if (done && ++sk == NSK) { sk = 0; pk ^= 1; }
-                return true;
+            }
+            pp ^= 1u << x;
+            if (stage_done) {
+                if (leader) tc_commit(bar(X_VEMPTY) + 8u * sv);
+                if (++sv == NSV) { sv = 0; pv ^= 1; }
+            }
+        };
+        // An alternate segment's next score, if it may be issued (wait_for_it: as soon as it may).
+        auto alt_score = [&](int j, int n, bool wait_for_it) {
+            auto have = [&](int i, uint32_t parity) {
+                return wait_for_it ? wait(i, parity) : __all_sync(0xffffffffu, mbar_test(bar(i), parity)) != 0;
             };
-            if (alt) ok = mbar_wait_warp(bar(X_QALT) + 8u * qr, (qa >> qr) & 1, abort_flag);
-            for (int x = 0; x < 2 && x < ops && ok; ++x) {
-                if (!alt) ok = mbar_wait_warp(bar(X_QWIDE + x), qw, abort_flag);
-                if (ok) ok = score(x, alt ? x == ops - 1 : ops == 2);
-            }
-            for (int j = 0; j < ops && ok; ++j) {          // O_x += P_x V(step), half of the tokens as soon as their P is there
-                const int x = j & 1;
-                const uint32_t vb = v0 + sv * (STAGE >> 4);
-                if (alt || x == 0) ok = mbar_wait_warp(bar(X_VFULL) + 8u * sv, pv, abort_flag);
-                // (a segment's first PV product starts a fresh O: the last segment's must have been read)
-                if (ok && j < 2 && seg > 0) ok = mbar_wait_warp(bar(X_OFREE + x), (seg - 1) & 1, abort_flag);
+            if ((j == 0 && !have(X_QALT + (int)qr, (qa >> qr) & 1)) || !have(X_KFULL + (int)sk, pk)) return 0;
+            score(sx, qr, true, j + 1 == n);
+            if (j + 1 == n) { qa ^= 1u << qr; qr ^= 1; }
+            sx ^= 1;
+            return 1;
+        };
+        int n, n1, scored = 0;                             // steps of this segment and of the next, scores of this one issued so far
+        bool alt, alt1;
+        fetch(n, alt);
+        while (ok && n > 0) {
+            int scored1 = 0;
+            if (alt) {
+                while (ok && scored < 2 && scored < n) scored += alt_score(scored, n, true);
+                fetch(n1, alt1);
+                for (int j = 0; j < n && ok; ++j) {
+                    if (!wait(X_VFULL + (int)sv, pv)) break;
+                    product(px, j < 2, true);
+                    if (!ok) break;
+                    if (j + 2 >= n && leader) tc_commit(bar(X_OFULL + px));
+                    px ^= 1;
+                    // the tile's next score (overwrites P of this operation, which the product before it reads): of this segment, or of
+                    // the next one where that is an alternate one (a wide one's Q rows come from threads that first have to end this
+                    // segment) and its operands are there already (a wait here would hold up this segment's products)
+                    if (scored < n) scored += alt_score(scored, n, true);
+                    else if (alt1 && scored1 < n1) scored1 += alt_score(scored1, n1, false);
+                }
+                // (a tile without an operation keeps step as well: neither side may be two phases ahead of the other)
+                if (ok && n == 1) {
+                    if (seg == 0 || wait(X_OFREE + px, (seg - 1) & 1)) { if (leader) tc_commit(bar(X_OFULL + px)); }
+                }
+            } else {
+                for (int x = 0; x < 2 && ok; ++x)
+                    if (wait(X_QWIDE + x, qw) && (x == 1 || wait(X_KFULL + (int)sk, pk))) score(x, x, x == 1, n == 1);
+                qw ^= 1;
+                fetch(n1, alt1);
+                for (int t = 0; t < n && ok; ++t) {
+                    if (!wait(X_VFULL + (int)sv, pv)) break;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (!ok || !(ok = mbar_wait_warp(bar(X_PFULL + 2 * x + h), (pp >> x) & 1, abort_flag))) break;
-                    tc_fence_after();
-                    if (leader) {
-#pragma unroll
-                        for (int ks = h * (STEP / 32); ks < (h + 1) * (STEP / 32); ++ks)
-                            tc_mma_ts(tmem + COL_O + x * 128, tmem + COL_S + x * 128 + ks * 8, vb + ks * 128, DESC_HI, IDESC_O, (j > 1 || ks > 0) ? 1u : 0u);
+                    for (int x = 0; x < 2; ++x) {
+                        if (!ok) break;
+                        product(x, t == 0, x == 1);
+                        if (!ok) break;
+                        if (t + 1 < n) {                   // overwrites P of this step, which the product before it reads
+                            if (x == 1 || wait(X_KFULL + (int)sk, pk)) score(x, x, x == 1, t + 2 == n);
+                        } else if (leader) {
+                            tc_commit(bar(X_OFULL + x));
+                        }
                     }
                 }
-                if (!ok) break;
-                pp ^= 1u << x;
-                if (alt || x == 1) {
-                    if (leader) tc_commit(bar(X_VEMPTY) + 8u * sv);
-                    if (++sv == NSV) { sv = 0; pv ^= 1; }
-                }
-                if (j + 2 < ops) ok = score(x, alt ? j + 3 == ops : j + 4 >= ops);   // overwrites P of this operation, which the product before it reads
-                else if (leader) tc_commit(bar(X_OFULL + x));
+                sx = px = 0;
             }
-            // (a tile without an operation keeps step as well: neither side may be two phases ahead of the other)
-            if (ok && ops == 1) {
-                if (seg > 0) ok = mbar_wait_warp(bar(X_OFREE + 1), (seg - 1) & 1, abort_flag);
-                if (ok && leader) tc_commit(bar(X_OFULL + 1));
-            }
-            if (alt) { qa ^= 1u << qr; qr ^= 1; } else qw ^= 1;
             ++seg;
+            n = n1; alt = alt1; scored = scored1;
         }
         __syncwarp();
     } else if (warp == 3) {
@@ -378,33 +435,41 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t lane_addr = tmem + ((uint32_t)(32 * sp) << 16);
         const uint32_t s_addr = lane_addr + COL_S + x * 128, o_addr = lane_addr + COL_O + x * 128;
         pdl_wait();                                           // q, tree_mask and every output come after the preceding kernel
+        pdl_launch_dependents();                              // (few_rows_kernel, which may follow, reads q ahead of its own wait)
         const int G = p.G, N = p.N;
         PIter si = make_iter();
         PSeg sg;
-        int it = 0, steps_before = 0;                         // operations of this tile so far / steps of all segments so far
+        int it = 0, steps_before = 0, x0 = 0;                 // operations of this tile so far / steps of all segments so far / tile that begins
         uint32_t o_phase = 0;
         int fills[2] = {0, 0}, qr = 0;                        // how often each Q region has been filled; the next alternate segment's
         bool ok = true;
-        while (ok && si.next(sg)) {
-            const int tile0 = sg.alt ? 0 : x * 128;           // this tile's first row in the unit
-            // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage.  Thread t moves chunk t % 16 of rows
-            // t / 16, t / 16 + 8, ... (a loop of little code: unrolled with its divisions it took 8000 cycles, most of them the fetch of its code)
+        // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage, asked for here and handed over by q_here.
+        // Thread t moves chunk t % 16 of rows t / 16, t / 16 + 8, ... (a loop of little code: unrolled with its divisions it took 8000
+        // cycles, most of them the fetch of its code).  Rows that do not exist keep what is there: a row's scores are its own.
+        auto q_ask = [&]() {
             if (sg.alt) {
                 if (qr) ++fills[1]; else ++fills[0];
                 qr ^= 1;
-            } else {
-                if (!(ok = mbar_wait_warp(bar(X_QEMPTY + x), ((x ? fills[1] : fills[0]) & 1) ^ 1, abort_flag))) break;
-                ++fills[0]; ++fills[1];
-                const int c = tl & 15, step_nd = 8 / G, step_g = 8 % G;
-                const uint32_t dst = base + R::OFF_Q + x * STAGE + (c >> 3) * HALF_BYTES;
-                int nd = sg.node0 + (sg.rows0 + tile0 + (tl >> 4)) / G, g = (sg.rows0 + tile0 + (tl >> 4)) % G;
+                return;
+            }
+            if (!(ok = mbar_wait_warp(bar(X_QEMPTY + x), ((x ? fills[1] : fills[0]) & 1) ^ 1, abort_flag))) return;
+            ++fills[0]; ++fills[1];
+            const int c = tl & 15, step_nd = 8 / G, step_g = 8 % G, row0 = sg.rows0 + x * 128 + (tl >> 4), end = min(128, sg.rows - x * 128);
+            const uint32_t dst = base + R::OFF_Q + x * STAGE + (c >> 3) * HALF_BYTES;
+            int nd = sg.node0 + row0 / G, g = row0 % G;
 #pragma unroll 2
-                for (int r = tl >> 4; r < min(128, sg.rows - tile0); r += 8) {     // (rows that do not exist keep what is there)
-                    cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + ((size_t)nd * p.Hq + sg.kvh * G + g) * D + c * 8);
-                    nd += step_nd;
-                    g += step_g;
-                    if (g >= G) { g -= G; ++nd; }
-                }
+            for (int r = tl >> 4; r < end; r += 8) {
+                cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), p.q + ((size_t)nd * p.Hq + sg.kvh * G + g) * D + c * 8);
+                nd += step_nd;
+                g += step_g;
+                if (g >= G) { g -= G; ++nd; }
+            }
+        };
+        bool live = si.next(sg);
+        if (live) q_ask();
+        while (ok && live) {
+            const int tile0 = sg.alt ? 0 : x * 128;           // this tile's first row in the unit
+            if (!sg.alt) {
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_async_smem();
                 mbar_arrive(bar(X_QWIDE + x));
@@ -424,7 +489,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             float m_ref = -INFINITY, l_run = 0.f;
             bool has_o = false;
 
-            for (int t = sg.alt ? x : 0; t < sg.n; t += sg.alt ? 2 : 1, ++it) {
+            for (int t = sg.alt ? x ^ x0 : 0; t < sg.n; t += sg.alt ? 2 : 1, ++it) {
                 const int tok0 = (sg.st0 + t) * STEP;
                 // (this product was issued after the tile's last PV product, so that one is complete too: O and the columns of P are free)
                 if (!mbar_wait_warp(bar(X_SFULL + x), it & 1, abort_flag)) { ok = false; break; }
@@ -435,12 +500,11 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     // the product (wide: both tiles' warps write them, whichever product comes first)
                     const int sv = (steps_before + t) % NSV;
                     fail = !mbar_wait(bar(X_VFULL + sv), ((steps_before + t) / NSV) & 1, abort_flag);
-                    if (!fail && tok0 + tl >= total) {
-                        unsigned char* vrow = sm + R::OFF_V + sv * STAGE + tl * 128;
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            *reinterpret_cast<uint4*>(vrow + c * 16) = make_uint4(0, 0, 0, 0);
-                            *reinterpret_cast<uint4*>(vrow + HALF_BYTES + c * 16) = make_uint4(0, 0, 0, 0);
+                    if (!fail) {                              // (consecutive threads write consecutive vectors: a row per thread met one bank)
+                        unsigned char* v0 = sm + R::OFF_V + sv * STAGE;
+                        for (int i = (total - tok0) * 8 + tl; i < STEP * 8; i += 128) {
+                            *reinterpret_cast<uint4*>(v0 + i * 16) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(v0 + HALF_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
                         }
                     }
                     fence_async_smem();
@@ -453,24 +517,33 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     has_o = true;
                     continue;
                 }
-                // The row is read from tensor memory in halves of 64 columns, the upper half twice (see attn_tc5_wide.cu).
-                const bool tail = tok0 + STEP > S;                  // reaches past the committed keys: mask bits
-                uint64_t a0 = 0, a1 = 0;                            // bit c of (a0, a1): column c may be attended to
-                if (tail) {
+                if (tok0 + STEP > S) {
+                    // reaches past the committed keys: columns that the row must not see become -inf in tensor memory, so that the
+                    // passes below know nothing of masks (in each of them, unrolled, a masked step took 2000 cycles more)
+                    uint64_t a0, a1;                                // bit c of (a0, a1): column c may be attended to
                     const int t0 = tok0 - S;
                     if (t0 >= 0) shr128(mk0, mk1, t0, a0, a1); else shl128_fill(mk0, mk1, -t0, a0, a1);
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        const uint64_t a = c & 2 ? a1 : a0;
+                        const uint32_t w = (uint32_t)(c & 1 ? a >> 32 : a);
+                        if (__all_sync(0xffffffffu, w == 0xffffffffu)) continue;
+                        uint32_t v[32];
+                        tmem_ld32(s_addr + c * 32, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!((w >> e) & 1u)) v[e] = 0xff800000u;
+                        tmem_st32(s_addr + c * 32, v);
+                    }
+                    tmem_wait_st();
                 }
+                // The row is read from tensor memory in halves of 64 columns, the upper half twice (see attn_tc5_wide.cu).
                 uint32_t s[64];
                 auto load_half = [&](int h) {
                     tmem_ld32(s_addr + h * 64, s);
                     tmem_ld32(s_addr + h * 64 + 32, s + 32);
                     tmem_wait_ld();
-                    if (tail) {
-                        const uint64_t a = h ? a1 : a0;
-#pragma unroll
-                        for (int c = 0; c < 64; ++c)
-                            if (!((a >> c) & 1ull)) s[c] = 0xff800000u;
-                    }
                 };
                 float mx[8];
 #pragma unroll
@@ -532,17 +605,21 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             if (!ok) break;
             steps_before += sg.n;
+            const int piece = sg.alt ? x ^ x0 : x;                // (an alternate unit of one step has only the piece of the tile that began)
+            x0 = sg.alt ? x0 ^ (sg.n & 1) : 0;
 
-            // ---- segment epilogue: the row's partial ----
-            if (!(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
+            // ---- segment epilogue: the row's partial; the next segment's Q rows are asked for first ----
+            const int rows2 = 2 * p.half[sg.kind];
+            float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * rows2 + piece * (rows2 >> 1) + tl;
+            if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * rows2 + piece * (rows2 >> 1) + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
+            live = si.next(sg);
+            if (live) q_ask();
+            if (!ok || !(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
             o_phase ^= 1;
             tc_fence_after();
             // O is free for the next segment's products as soon as it has been read, ahead of the last stores.  (No partial is read before
             // this kernel has ended, so the arrival need not wait for them.)
             if (warp_rows) {
-                const int rows2 = 2 * p.half[sg.kind];
-                float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * rows2 + x * (rows2 >> 1) + tl;
-                if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * rows2 + x * (rows2 >> 1) + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
@@ -605,10 +682,9 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
         n[kind] = 0;
         if (steps == 0) continue;
         alt[kind] = rows <= 128;
-        const int w = m == nb - 1 ? p.last_w[kind] : kWideStep;
-        const int u0 = (kind ? base_b : 0) + kvh * head_places(p, kind, steps) + m * unit_places(p, kind, steps, false) + kSegStart;
+        const int u0 = (kind ? base_b : 0) + kvh * head_places(p, kind, steps) + m * unit_places(p, kind, steps, false) + start_places(alt[kind]);
         c0[kind] = u0 / R;
-        const int c1 = (u0 + (steps - 1) * w) / R;
+        const int c1 = (u0 + (steps - 1) * step_places(alt[kind])) / R;
         n[kind] = (c1 - c0[kind] + 1) * (alt[kind] ? 2 : 1);
         if (steps == 1) n[kind] = 1;                          // (an alternate unit of one step: the second tile has nothing)
         const int unit = kind ? (b * p.Hkv + kvh) * nb + m : kvh * nb + m;
@@ -718,7 +794,7 @@ bool attn_prefix_supports(const AttnArgs& a, int prefix) {
     long long T = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const long long steps = ((kind ? (long long)a.S_max - prefix : prefix) + STEP - 1) / STEP;
-        T += (kind ? (long long)a.B : 1) * a.Hkv * l.blocks[kind] * (kSegStart + steps * kWideStep);
+        T += (kind ? (long long)a.B : 1) * a.Hkv * l.blocks[kind] * (kWideStart + steps * kWideStep);
         if (l.slots[kind] * 2 * l.half[kind] >= (1ll << 31)) return false;
     }
     return T < (1ll << 31) - (1 << 20);
@@ -734,12 +810,12 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         p.part_o[kind] = (float4*)ws;
         ws += (size_t)l.slots[kind] * 2 * l.half[kind] * D * 4;
         p.half[kind] = l.half[kind]; p.blocks[kind] = l.blocks[kind];
-        p.last_w[kind] = l.rows[kind] - (l.blocks[kind] - 1) * kRows <= 128 ? kAltStep : kWideStep;
+        p.last_alt[kind] = l.rows[kind] - (l.blocks[kind] - 1) * kRows <= 128;
     }
     for (int kind = 0; kind < 2; ++kind) { p.part_ml[kind] = (float2*)ws; ws += (size_t)l.slots[kind] * 2 * l.half[kind] * 8; }
     p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv;
     p.P = prefix; p.cap = a.S_max - prefix;
-    p.early = a.early_prefetch ? 1 : 0; p.grid = a.sm_count;
+    p.early = a.early_prefetch ? 1 : 0; p.grid = a.sm_count; p.groups = a.B;
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.status = a.status;
     const PagedArgs pa = {a.block_table, a.table_stride, a.page_rows, a.num_blocks, a.Hkv, a.N, a.token_major, a.status, nullptr};
