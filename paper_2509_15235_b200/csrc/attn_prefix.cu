@@ -82,7 +82,7 @@ struct PrefixParams {
 
 // Places of the line (some 210 cycles each, from clock stamps of 8 x 60 nodes of 32/32 heads): a wide step 3400 cycles, an alternate
 // one 1900, the start of a segment (Q rows, first score, last product, partials) 7500 and 3500.
-constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 48;
+constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 28;
 __host__ __device__ constexpr int step_places(bool alt) { return alt ? kAltStep : kWideStep; }
 __host__ __device__ constexpr int start_places(bool alt) { return alt ? kAltStart : kWideStart; }
 
@@ -752,6 +752,285 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
     if (S < 0 && cg == 0 && r == 0 && kvh == 0) atomicCAS(p.status, 0, (int)VISPEC_E_RANGE);
 }
 
+// ------------------------------------------------------------------------------------------------
+// Few rows per unit (N * G <= 16: single tokens, small trees): the sequences' own keys, and the join with the prefix.
+//
+// What bounds it: the read of the own keys.  A tile of 128 rows would be nearly empty and its segments would cost more to start than
+// to stream (32 sequences x 40 heads with one row each: 8 segments per SM of 8 to 10 thousand cycles), so here a warp takes 16 keys at
+// a time on its own, by asynchronous 16-byte copies two or three groups deep into shared memory of its own, and has nothing to set up:
+//   S = Q K^T   (mma.sync m16n8k16) lane (key k = lane / 4, part q = lane % 4) reads 16 bytes of key k at elements 32 j + 8 q: the pairs
+//               are the B operand of two products whose 16 contracted elements are 32 j + 8 q' + 4 s + {0, 1} and + {2, 3}; Q alike.
+//   O += P V    P is S's accumulator layout read as an A operand.  The lane reads 16 bytes of keys 2q, 2q + 1, 2q + 8, 2q + 9 at
+//               elements 64 h + 8 (lane / 4); column c of product (h, t) is element 64 h + 8 c + t, so a lane's accumulators are 16
+//               consecutive elements of each half of its rows.
+// (Loaded straight into registers instead, 12 warps of 168 registers per SM reached 3.7 TB/s: a warp then either loads or computes.)
+// A unit is a warp's, or that of 2 or 4 warps of a block, or where units are few of a cluster of 2, 4 or 8 blocks; they take the groups
+// of 16 keys and the prefix's pieces in turn, their (m, l, o) meet in shared memory and the row is finished here.
+// ------------------------------------------------------------------------------------------------
+constexpr int kFewWarps = 4, kFewRows = 16;
+constexpr int kFewStage = 2 * 16 * D * 2;          // bytes of 16 keys and their values
+// Blocks of eight rows -> stages of a warp, blocks on an SM: the registers decide.
+__host__ __device__ constexpr int few_stages(int r) { return r == 1 ? 2 : 3; }
+__host__ __device__ constexpr int few_smem(int r) { return kFewWarps * few_stages(r) * kFewStage; }
+
+__device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// R: blocks of 8 rows that exist (1 or 2).
+template <int R>
+__global__ void __launch_bounds__(32 * kFewWarps, R == 1 ? 3 : 2)
+few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ PagedArgs pa, const uint4* __restrict__ k_pool,
+                const uint4* __restrict__ v_pool, const int wpu /* warps of a block that share a unit */) {
+    constexpr int ROWS = 8 * R, kFewStages = few_stages(R);
+    extern __shared__ __align__(1024) unsigned char sm[];
+    __shared__ float2 park_ml[kFewWarps][ROWS];
+    static_assert(ROWS * (D / 4 + 1) * 16 <= kFewStages * kFewStage, "a warp's part does not fit its stages");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q4 = lane & 3, c8 = lane >> 2;
+    const int ck = (int)cluster_size(), cr = (int)cluster_ctarank();
+    const int sub = warp % wpu, first_warp = warp - sub, units = p.B * p.Hkv;
+    const int unit_ = ck > 1 ? blockIdx.x / ck : (blockIdx.x * kFewWarps + warp) / wpu;
+    const bool live = unit_ < units;               // (the last block may have warps without a unit)
+    const int unit = live ? unit_ : units - 1, b = unit / p.Hkv, kvh = unit - b * p.Hkv;
+    const int wi = ck > 1 ? cr * kFewWarps + warp : sub, nw = ck > 1 ? ck * kFewWarps : wpu;
+    const int RG = p.N * p.G, W = (p.N + 63) >> 6;
+    if (!p.early) pdl_wait();
+    pdl_launch_dependents();
+    const int S = own_len(p, p.kv_len[b]), total = S + p.N;
+    const bool good = S >= 0;
+    // Rows of this lane: c8 and, with R == 2, c8 + 8.  (q, tree_mask and the tree's own keys: the kernel before has waited for what
+    // writes them before it let this one in; where there is none, this one waits.)
+    if (p.early && p.P == 0) pdl_wait();
+    uint32_t qa[D / 16][2 * R];                    // [j * 2 + s]: A registers (row, row + 8) x (first, second half of the 16 elements)
+    uint64_t mk[R][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = c8 + 8 * r;
+        const bool there = row < RG;
+        const int node = there ? row / p.G : 0, head = kvh * p.G + (there ? row % p.G : 0);
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (((size_t)b * p.N + node) * p.Hq + head) * D) + q4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint4 v = there ? __ldcg(src + 4 * j) : make_uint4(0, 0, 0, 0);
+            qa[2 * j][r] = v.x; qa[2 * j][R + r] = v.y; qa[2 * j + 1][r] = v.z; qa[2 * j + 1][R + r] = v.w;
+        }
+        mk[r][0] = mk[r][1] = 0;
+        if (there) {
+            const uint64_t* mrow = p.mask + ((size_t)b * p.N + node) * W;
+            mk[r][0] = __ldcg(mrow);
+            if (W > 1) mk[r][1] = __ldcg(mrow + 1);
+        }
+    }
+    float o[16][2 * R], m_ref[R], l_run[R];        // o[t + 8 h][2 r + i]: row c8 + 8 r, element 64 h + 8 (2 q4 + i) + t
+#pragma unroll
+    for (int t = 0; t < 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 2 * R; ++i) o[t][i] = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) { m_ref[r] = -INFINITY; l_run[r] = 0.f; }
+
+    // ---- own keys: groups of 16, number i of this warp is wi + i * nw ----
+    const int groups = good && live ? (total + 15) / 16 : 0, mine_n = groups > wi ? (groups - wi + nw - 1) / nw : 0;
+    const int32_t* trow = pa.block_table + (size_t)b * pa.table_stride + p.P / pa.page_rows;
+    const size_t stride = (size_t)(pa.token_major ? pa.Hkv : 1) * (D / 8);                  // 16-byte vectors between keys
+    const size_t head_at = (size_t)kvh * (pa.token_major ? 1 : pa.page_rows) * (D / 8);
+    const size_t block = (size_t)pa.page_rows * pa.Hkv * (D / 8);
+    unsigned char* const mine = sm + warp * kFewStages * kFewStage;
+    const uint32_t mine_at = smem_u32(mine);
+    // the table's entries of the warp's groups 32 i .. 32 i + 31, asked for ahead of kv_len
+    auto entries_at = [&](int i) {
+        const int at = (wi + (i + lane) * nw) * 16 / pa.page_rows;
+        return at < pa.table_stride - p.P / pa.page_rows ? trow[at] : -1;
+    };
+    int entries = entries_at(0);
+    // Group i on its way into stage i % kFewStages: half a warp per key, 16-byte chunks exchanged so that the reads below
+    // meet every bank once.  Keys past the last one (their rows may hold anything) and entries outside the pool become zeros.
+    auto fetch = [&](int i) {
+        if (i < mine_n) {
+            if (i > 0 && (i & 31) == 0) entries = entries_at(i);
+            const int e = __shfl_sync(0xffffffffu, entries, i & 31), key0 = (wi + i * nw) * 16;
+            const bool in_pool = e >= 0 && e < pa.num_blocks;
+            if (!in_pool && lane == 0 && p.status) atomicCAS(p.status, 0, (int)VISPEC_E_RANGE);
+            const int c = lane & 15, r0 = lane >> 4;
+            const size_t at = (in_pool ? (size_t)e : 0) * block + head_at + (size_t)(key0 % pa.page_rows + r0) * stride + c;
+            const uint32_t dst = mine_at + (uint32_t)(i % kFewStages) * kFewStage;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = 2 * k + r0, n = in_pool && key0 + r < total ? 16 : 0;
+                const size_t from = n ? at + 2 * k * stride : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * 256 + ((c ^ (4 * (r & 1))) << 4)), "l"(k_pool + from), "r"(n) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + kFewStage / 2 + r * 256 + ((c ^ (2 * ((r >> 1) & 3))) << 4)), "l"(v_pool + from), "r"(n) : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kFewStages - 1; ++i) fetch(i);
+    for (int i = 0; i < mine_n; ++i) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+        __syncwarp();                              // everybody's copies of this group are here, and nobody reads the last one any more
+        fetch(i + kFewStages - 1);
+        const int key0 = (wi + i * nw) * 16;
+        const unsigned char* ks = mine + i % kFewStages * kFewStage;
+        const unsigned char* vs = ks + kFewStage / 2;
+        float sc[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 kk = *reinterpret_cast<const uint4*>(ks + (8 * n + c8) * 256 + (((4 * j + q4) ^ (4 * (c8 & 1))) << 4));
+                const uint32_t a0[4] = {qa[2 * j][0], R > 1 ? qa[2 * j][R - 1] : 0u, qa[2 * j][R], R > 1 ? qa[2 * j][2 * R - 1] : 0u};
+                const uint32_t a1[4] = {qa[2 * j + 1][0], R > 1 ? qa[2 * j + 1][R - 1] : 0u, qa[2 * j + 1][R], R > 1 ? qa[2 * j + 1][2 * R - 1] : 0u};
+                mma_16816(sc[n], a0, kk.x, kk.y);
+                mma_16816(sc[n], a1, kk.z, kk.w);
+            }
+        }
+        uint32_t pr[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[4] = {sc[0][2 * r], sc[0][2 * r + 1], sc[1][2 * r], sc[1][2 * r + 1]};   // keys 2q, 2q+1, 2q+8, 2q+9
+            if (key0 + 16 > S) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = key0 + 2 * q4 + (i & 1) + 8 * (i >> 1) - S;               // tree node of this key, if it is one
+                    const uint64_t w = t >= 64 ? mk[r][1] : mk[r][0];
+                    if (t >= 0 && !(t < p.N && (w >> (t & 63)) & 1ull)) x[i] = -INFINITY;
+                }
+            }
+            float top = max_nan(max3_nan(x[0], x[1], x[2]), x[3]);
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2)) * p.scale_log2;
+            if (top > m_ref[r] + kRescaleGap) {                                              // also on the first finite group
+                const float a = exp2f(m_ref[r] - top);
+                m_ref[r] = top;
+                l_run[r] *= a;
+#pragma unroll
+                for (int t = 0; t < 16; ++t) { o[t][2 * r] *= a; o[t][2 * r + 1] *= a; }
+            }
+            if (!(top < INFINITY)) l_run[r] = top - top;                                     // a NaN or an infinite score (see inv_sum)
+            const float m_use = m_ref[r] == -INFINITY ? 0.f : m_ref[r];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = exp2f(fmaf(x[i], p.scale_log2, -m_use));
+            l_run[r] += (x[0] + x[1]) + (x[2] + x[3]);                                       // this lane's keys; summed over the lanes below
+            pr[r] = pack_bf16(x[0], x[1]);
+            pr[2 + r] = pack_bf16(x[2], x[3]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t v[4][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint4 u = *reinterpret_cast<const uint4*>(vs + (2 * q4 + (x & 1) + 8 * (x >> 1)) * 256 + (((8 * h + c8) ^ (2 * q4)) << 4));
+                v[x][0] = u.x; v[x][1] = u.y; v[x][2] = u.z; v[x][3] = u.w;
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const uint32_t sel = t & 1 ? 0x7632u : 0x5410u;
+                float c[4] = {o[8 * h + t][0], o[8 * h + t][1], R > 1 ? o[8 * h + t][2 * R - 2] : 0.f, R > 1 ? o[8 * h + t][2 * R - 1] : 0.f};
+                mma_16816(c, pr, __byte_perm(v[0][t >> 1], v[1][t >> 1], sel), __byte_perm(v[2][t >> 1], v[3][t >> 1], sel));
+                o[8 * h + t][0] = c[0]; o[8 * h + t][1] = c[1];
+                if (R > 1) { o[8 * h + t][2 * R - 2] = c[2]; o[8 * h + t][2 * R - 1] = c[3]; }
+            }
+        }
+    }
+    __syncwarp();                                  // (the stages take the warp's part below)
+    // (a NaN or infinite score was seen by all lanes of the row, so every lane's l is NaN then)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
+        l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 2);
+        if (!(l_run[r] > 0.f)) m_ref[r] = -INFINITY;
+    }
+
+    // ---- the prefix's pieces of these rows, from the kernel before ----
+    if (p.early && p.P > 0) pdl_wait();
+    if (good && live && p.P > 0) {
+        const int steps = steps_of(p.P), Rg = range_of(p.Hkv * head_places(p, 0, steps), p.grid), rows2 = 2 * p.half[0];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int row = b * RG + min(c8 + 8 * r, RG - 1), m = row / kRows, lr = row - m * kRows, nb = p.blocks[0];
+            const bool alt = min(kRows, p.B * RG - m * kRows) <= 128;
+            const int u0 = kvh * head_places(p, 0, steps) + m * unit_places(p, 0, steps, false) + start_places(alt);
+            const int first = u0 / Rg, last = (u0 + (steps - 1) * step_places(alt)) / Rg;
+            const int pieces = (last - first + 1) * (alt ? 2 : 1);
+            for (int e = wi; e < pieces; e += nw) {
+                const int slot = kvh * nb + m + first + (alt ? e >> 1 : e), in = alt ? (e & 1) * p.half[0] + lr : lr;
+                const float2 ml = __ldcg(p.part_ml[0] + (size_t)slot * rows2 + in);
+                const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows2 + in;
+                float4 v[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows2);
+                const float m_new = fmaxf(m_ref[r], ml.x), m_use = m_new == -INFINITY ? 0.f : m_new;
+                const float a = exp2f(m_ref[r] - m_use), w = exp2f(ml.x - m_use);
+                l_run[r] = l_run[r] * a + ml.y * w;
+                m_ref[r] = m_new;
+                if (ml.x == -INFINITY) continue;                                             // (its o may never have been written)
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {                                                // elements 64 h + 16 q4 + 4 (x & 3) + 0..3
+                    const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
+                    o[8 * h + t][2 * r + i] = o[8 * h + t][2 * r + i] * a + v[x].x * w;
+                    o[8 * h + t + 1][2 * r + i] = o[8 * h + t + 1][2 * r + i] * a + v[x].y * w;
+                    o[8 * h + t + 2][2 * r + i] = o[8 * h + t + 2][2 * r + i] * a + v[x].z * w;
+                    o[8 * h + t + 3][2 * r + i] = o[8 * h + t + 3][2 * r + i] * a + v[x].w * w;
+                }
+            }
+        }
+    }
+
+    // ---- the warps' parts meet ----
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
+            reinterpret_cast<float4*>(mine)[(c8 + 8 * r) * (D / 4 + 1) + 16 * h + 4 * q4 + (x & 3)] =
+                make_float4(o[8 * h + t][2 * r + i], o[8 * h + t + 1][2 * r + i], o[8 * h + t + 2][2 * r + i], o[8 * h + t + 3][2 * r + i]);
+        }
+        if (q4 == 0) park_ml[warp][c8 + 8 * r] = make_float2(m_ref[r], l_run[r]);
+    }
+    if (ck > 1) cluster_sync_all(); else if (wpu > 1) __syncthreads(); else __syncwarp();
+    const uint32_t o_at = smem_u32(sm), ml_at = smem_u32(&park_ml[0][0]);
+    // thread <-> (row, 4 columns); the ranks of a cluster take rows in turn
+    for (int item = wi * 32 + lane; live && item < RG * (D / 4); item += nw * 32) {
+        const int row = item / (D / 4), c4 = item % (D / 4);
+        float m_all = -INFINITY, l_all = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < ck; ++k) {
+            float2 ml[kFewWarps];
+            float4 v[kFewWarps];
+            const uint32_t po = ck > 1 ? dsmem_addr(o_at, k) : o_at, pm = ck > 1 ? dsmem_addr(ml_at, k) : ml_at;
+#pragma unroll
+            for (int x = 0; x < kFewWarps; ++x) {
+                const int w = first_warp + x;
+                ml[x] = make_float2(-INFINITY, 0.f);
+                v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (x >= wpu) continue;
+                const uint32_t om = (uint32_t)((w * ROWS + row) * 8), oo = (uint32_t)(w * kFewStages * kFewStage + (row * (D / 4 + 1) + c4) * 16);
+                ml[x] = ck > 1 ? dsmem_ld2(pm + om) : smem_ld2(pm + om);
+                v[x] = ck > 1 ? dsmem_ld4(po + oo) : smem_ld4(po + oo);
+            }
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float m_new = fmaxf(m_all, ml[w].x), m_use = m_new == -INFINITY ? 0.f : m_new;
+                const float a = exp2f(m_all - m_use), u = exp2f(ml[w].x - m_use);
+                l_all = l_all * a + ml[w].y * u;
+                acc.x = acc.x * a + v[w].x * u; acc.y = acc.y * a + v[w].y * u; acc.z = acc.z * a + v[w].z * u; acc.w = acc.w * a + v[w].w * u;
+                m_all = m_new;
+            }
+        }
+        const int node = row / p.G, head = kvh * p.G + row % p.G;
+        const float inv = inv_sum(l_all);
+        *reinterpret_cast<uint2*>(p.out + (((size_t)b * p.N + node) * p.Hq + head) * D + c4 * 4) =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (p.lse && c4 == 0)
+            p.lse[((size_t)b * p.Hq + head) * p.N + node] = l_all > 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+    }
+    if (!good && kvh == 0 && wi == 0 && lane == 0) atomicCAS(p.status, 0, (int)VISPEC_E_RANGE);
+    if (ck > 1) cluster_sync_all();                // nobody leaves while a peer may still read its shared memory
+}
+
 // What of the scratch a call of B sequences of N nodes uses.
 struct PrefixLayout {
     int rows[2], blocks[2], half[2];
@@ -782,6 +1061,11 @@ cudaError_t init_attn_prefix() {
     const void* merges[2] = {(const void*)prefix_merge_kernel<1>, (const void*)prefix_merge_kernel<4>};
     for (const void* m : merges) {                    // (see init_merge)
         const cudaError_t e = cudaFuncSetAttribute(m, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (e != cudaSuccess) return e;
+    }
+    for (int r = 1; r <= 2; ++r) {
+        const cudaError_t e = cudaFuncSetAttribute(r == 1 ? (const void*)few_rows_kernel<1> : (const void*)few_rows_kernel<2>,
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(r));
         if (e != cudaSuccess) return e;
     }
     return cudaFuncSetAttribute((const void*)attn_prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
@@ -819,9 +1103,28 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.status = a.status;
     const PagedArgs pa = {a.block_table, a.table_stride, a.page_rows, a.num_blocks, a.Hkv, a.N, a.token_major, a.status, nullptr};
-    cudaError_t err = launch_pdl(attn_prefix_kernel, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa);
-    if (err != cudaSuccess) return err;
-    ++*n_launches;
+    const bool few = l.rows[1] <= kFewRows;
+    if (few) p.groups = 0;
+    cudaError_t err = cudaSuccess;
+    if (!few || prefix > 0) {
+        err = launch_pdl(attn_prefix_kernel, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa);
+        if (err != cudaSuccess) return err;
+        ++*n_launches;
+    }
+    if (few) {
+        // Warps to a unit: as many as bring eight of them to every SM, as long as each has a group of keys.
+        const int units = a.B * a.Hkv, most = (p.cap + 15) / 16;
+        int nw = 1;
+        while (nw < 8 * kFewWarps && 2 * nw <= most && units * nw < 8 * a.sm_count) nw *= 2;
+        const int ck = nw > kFewWarps ? nw / kFewWarps : 1, wpu = nw > kFewWarps ? kFewWarps : nw;
+        const int blocks = ck > 1 ? units * ck : (units * wpu + kFewWarps - 1) / kFewWarps;
+        auto go = [&](auto kernel, int r) {
+            return launch_pdl(kernel, dim3(blocks), dim3(32 * kFewWarps), few_smem(r), st, ck, p, pa, (const uint4*)a.k, (const uint4*)a.v, wpu);
+        };
+        err = l.rows[1] <= 8 ? go(few_rows_kernel<1>, 1) : go(few_rows_kernel<2>, 2);
+        if (err == cudaSuccess) ++*n_launches;
+        return err;
+    }
     // One group of four columns per thread while that leaves the SMs with few threads, whole 32-byte sectors of the output beyond.
     const long long rows = (long long)a.B * a.N * a.Hq;
     const bool fine = rows * (D / 4) <= 1024ll * a.sm_count;
