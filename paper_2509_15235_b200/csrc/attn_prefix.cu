@@ -28,6 +28,7 @@
 // TMEM (512 columns): S_A 0..127, S_B 128..255 (P of the tile, bf16, in the first 64 columns of its S), O_A 256, O_B 384.
 // The waits, time-outs and the programmatic launch are those of attn_tc5.cu.
 #include <cuda_bf16.h>
+#include <algorithm>
 
 #include "tc5_common.cuh"
 
@@ -82,21 +83,21 @@ struct PrefixParams {
 
 // Places of the line (some 210 cycles each, from clock stamps of 8 x 60 nodes of 32/32 heads): a wide step 3400 cycles, an alternate
 // one 1900, the start of a segment (Q rows, first score, last product, partials) 7500 and 3500.
-constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 28;
+constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 36;
 __host__ __device__ constexpr int step_places(bool alt) { return alt ? kAltStep : kWideStep; }
 __host__ __device__ constexpr int start_places(bool alt) { return alt ? kAltStart : kWideStart; }
 
-__device__ __forceinline__ int unit_places(const PrefixParams& p, int kind, int steps, bool last) {
+__host__ __device__ __forceinline__ int unit_places(const PrefixParams& p, int kind, int steps, bool last) {
     const bool alt = last && p.last_alt[kind];
     return start_places(alt) + steps * step_places(alt);
 }
-__device__ __forceinline__ int head_places(const PrefixParams& p, int kind, int steps) {
+__host__ __device__ __forceinline__ int head_places(const PrefixParams& p, int kind, int steps) {
     return steps == 0 ? 0 : (p.blocks[kind] - 1) * unit_places(p, kind, steps, false) + unit_places(p, kind, steps, true);
 }
 __device__ __forceinline__ int own_len(const PrefixParams& p, int kv) {       // -1: rejected
     return kv >= p.P && kv - p.P <= p.cap - p.N ? kv - p.P : -1;
 }
-__device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
+__host__ __device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
 
 // One warp: exclusive sums of the sequences' places behind the prefix, and the range of a CTA.  store(b, base, len) for each sequence.
 template <typename F>
@@ -119,7 +120,7 @@ __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const
     }
     return carry;
 }
-__device__ __forceinline__ int range_of(int T, int grid) { return max((T + grid - 1) / grid, kMinRange); }
+__host__ __device__ __forceinline__ int range_of(int T, int grid) { return (T + grid - 1) / grid > kMinRange ? (T + grid - 1) / grid : kMinRange; }
 
 // The first step of a unit that starts at `start` whose place is at or behind g.
 __device__ __forceinline__ int step_at(int g, int start, bool alt) {
@@ -238,7 +239,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     if (warp == 3) {
         int kv[kMaxPrefixB / 32];
 #pragma unroll
-        for (int i = 0; i < kMaxPrefixB / 32; ++i) kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0;
+        for (int i = 0; i < kMaxPrefixB / 32; ++i) kv[i] = i * 32 + lane < p.groups ? p.kv_len[i * 32 + lane] : 0;
         const int T = line_build(p, lane, kv, [&](int, int b, int at, int S) {
             if (b < p.groups) { sched.base[b + 1] = at; sched.len[b] = S; }
         });
@@ -955,25 +956,34 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
             const int u0 = kvh * head_places(p, 0, steps) + m * unit_places(p, 0, steps, false) + start_places(alt);
             const int first = u0 / Rg, last = (u0 + (steps - 1) * step_places(alt)) / Rg;
             const int pieces = (last - first + 1) * (alt ? 2 : 1);
-            for (int e = wi; e < pieces; e += nw) {
-                const int slot = kvh * nb + m + first + (alt ? e >> 1 : e), in = alt ? (e & 1) * p.half[0] + lr : lr;
-                const float2 ml = __ldcg(p.part_ml[0] + (size_t)slot * rows2 + in);
-                const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows2 + in;
-                float4 v[8];
+            for (int e0 = wi; e0 < pieces; e0 += 2 * nw) {                                   // two at a time, their loads ahead of the sums
+                float2 ml[2];
+                float4 v[2][8];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows2);
-                const float m_new = fmaxf(m_ref[r], ml.x), m_use = m_new == -INFINITY ? 0.f : m_new;
-                const float a = exp2f(m_ref[r] - m_use), w = exp2f(ml.x - m_use);
-                l_run[r] = l_run[r] * a + ml.y * w;
-                m_ref[r] = m_new;
-                if (ml.x == -INFINITY) continue;                                             // (its o may never have been written)
+                for (int k = 0; k < 2; ++k) {
+                    const int e = e0 + k * nw < pieces ? e0 + k * nw : e0;
+                    const int slot = kvh * nb + m + first + (alt ? e >> 1 : e), in = alt ? (e & 1) * p.half[0] + lr : lr;
+                    ml[k] = __ldcg(p.part_ml[0] + (size_t)slot * rows2 + in);
+                    const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows2 + in;
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {                                                // elements 64 h + 16 q4 + 4 (x & 3) + 0..3
-                    const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
-                    o[8 * h + t][2 * r + i] = o[8 * h + t][2 * r + i] * a + v[x].x * w;
-                    o[8 * h + t + 1][2 * r + i] = o[8 * h + t + 1][2 * r + i] * a + v[x].y * w;
-                    o[8 * h + t + 2][2 * r + i] = o[8 * h + t + 2][2 * r + i] * a + v[x].z * w;
-                    o[8 * h + t + 3][2 * r + i] = o[8 * h + t + 3][2 * r + i] * a + v[x].w * w;
+                    for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows2);
+                }
+                if (e0 + nw >= pieces) ml[1] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float m_new = fmaxf(m_ref[r], ml[k].x), m_use = m_new == -INFINITY ? 0.f : m_new;
+                    const float a = exp2f(m_ref[r] - m_use), w = exp2f(ml[k].x - m_use);
+                    l_run[r] = l_run[r] * a + ml[k].y * w;
+                    m_ref[r] = m_new;
+                    if (ml[k].x == -INFINITY) continue;                                      // (its o may never have been written)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {                                            // elements 64 h + 16 q4 + 4 (x & 3) + 0..3
+                        const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
+                        o[8 * h + t][2 * r + i] = o[8 * h + t][2 * r + i] * a + v[k][x].x * w;
+                        o[8 * h + t + 1][2 * r + i] = o[8 * h + t + 1][2 * r + i] * a + v[k][x].y * w;
+                        o[8 * h + t + 2][2 * r + i] = o[8 * h + t + 2][2 * r + i] * a + v[k][x].z * w;
+                        o[8 * h + t + 3][2 * r + i] = o[8 * h + t + 3][2 * r + i] * a + v[k][x].w * w;
+                    }
                 }
             }
         }
@@ -1112,10 +1122,13 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         ++*n_launches;
     }
     if (few) {
-        // Warps to a unit: as many as bring eight of them to every SM, as long as each has a group of keys.
-        const int units = a.B * a.Hkv, most = (p.cap + 15) / 16;
+        // Warps to a unit: as many as the SMs hold at once, as long as each has a group of keys
+        // or a piece of the prefix.
+        const int units = a.B * a.Hkv, steps = steps_of(prefix), T = a.Hkv * head_places(p, 0, steps);
+        const int pieces = steps == 0 ? 0 : 2 * unit_places(p, 0, steps, true) / range_of(T, p.grid) + 1, most = std::max((p.cap + 15) / 16, pieces);
+        const int room = (l.rows[1] <= 8 ? 12 : 8) * a.sm_count;
         int nw = 1;
-        while (nw < 8 * kFewWarps && 2 * nw <= most && units * nw < 8 * a.sm_count) nw *= 2;
+        while (nw < 8 * kFewWarps && 2 * nw <= most && units * 2 * nw <= room) nw *= 2;
         const int ck = nw > kFewWarps ? nw / kFewWarps : 1, wpu = nw > kFewWarps ? kFewWarps : nw;
         const int blocks = ck > 1 ? units * ck : (units * wpu + kFewWarps - 1) / kFewWarps;
         auto go = [&](auto kernel, int r) {
