@@ -18,7 +18,7 @@
 // A segment runs on two accumulator tiles of 128 rows, each with four softmax warps, one thread per row, which work out of phase so that
 // the tensor pipe serves one while the other is in its exponentials, as in attn_tc5_wide.cu:
 //   wide        more than 128 rows: the tiles hold different rows and share every K/V stage
-//   alternate   at most 128 rows: both tiles hold the same rows and take turns at the steps, and a row has two pieces per segment
+//   alternate   at most 128 rows: both tiles hold the same rows and take turns at the steps; their parts meet at the segment's end
 // In terms of "operations" 0, 1, 2, ... (one tile's share of a step; the tiles take turns, across segments too) the issue order is
 // always S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ...
 //
@@ -40,12 +40,13 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kRows = 256;                     // query rows of a unit
+constexpr int kMaxLineB = 64;                  // sequences whose own keys are on the line (few_rows_kernel takes any number)
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;     // + 128 per tile
 
 enum { X_KFULL = 0, X_KEMPTY = X_KFULL + 2, X_VFULL = X_KEMPTY + 2, X_VEMPTY = X_VFULL + 3, X_SFULL = X_VEMPTY + 3,
        X_PFULL = X_SFULL + 2 /* [tile][half of the columns] */, X_QWIDE = X_PFULL + 4, X_QALT = X_QWIDE + 2, X_QEMPTY = X_QALT + 2,
-       X_OFULL = X_QEMPTY + 2, X_OFREE = X_OFULL + 2, X_COUNT = X_OFREE + 2 };
+       X_OFULL = X_QEMPTY + 2, X_OFREE = X_OFULL + 2, X_STAT = X_OFREE + 2, X_COUNT = X_STAT + 1 };
 
 struct PrefixRing {
     static constexpr int STAGE = 2 * HALF_BYTES, NSK = 2, NSV = 3;
@@ -53,26 +54,28 @@ struct PrefixRing {
     static constexpr int KFULL = X_KFULL, KEMPTY = X_KEMPTY, VFULL = X_VFULL, VEMPTY = X_VEMPTY;
 };
 constexpr int SMEM_BAR = 7 * PrefixRing::STAGE;
-constexpr int BAR_BYTES = 256;
+constexpr int BAR_BYTES = 240;
 static_assert(X_COUNT * 8 + 20 <= BAR_BYTES, "barrier block too small");
 constexpr int SMEM_SCHED = SMEM_BAR + BAR_BYTES;
 
 // Where things lie on the line.  Group 0 is the prefix, group b + 1 sequence b.
 struct PrefixSched {
-    int base[kMaxPrefixB + 2];     // where group g starts; base[B + 1] = length of the line
-    int len[kMaxPrefixB];          // sequence b's own committed slots; -1: rejected
+    int base[kMaxLineB + 2];       // where group g starts; base[groups + 1] = length of the line
+    int len[kMaxLineB];            // sequence b's own committed slots; -1: rejected
     int range;                     // places of the line per CTA
 };
 constexpr int SMEM_TABRING = SMEM_SCHED + ((int)sizeof(PrefixSched) + 15) / 16 * 16;
-constexpr int SMEM_ALLOC = SMEM_TABRING + 256;
+constexpr int SMEM_STAT = SMEM_TABRING + 256;   // (m, l) of both tiles' rows, exchanged at the end of an alternate segment
+constexpr int SMEM_ALLOC = SMEM_STAT + 256 * 8;
 static_assert(SMEM_ALLOC <= 232448, "over the 227 KB a CTA may have");
 
 struct PrefixParams {
     const __nv_bfloat16* q; const int32_t* kv_len; const uint64_t* mask;
     __nv_bfloat16* out; float* lse;
-    // partials: slot s of a region is [D/4][2 half] float4 and [2 half] (m, l); row r of tile x at x * half + r
+    // partials: slot s of a region is [D/4][slot_rows] float4 and [slot_rows] (m, l): the unit's rows, or where an alternate segment's
+    // parts are two pieces, the second one half the slot behind the first
     float4* part_o[2]; float2* part_ml[2];     // [0] prefix units, [1] sequences' own
-    int half[2], blocks[2], last_alt[2];       // rows per tile in a slot; row blocks per kv head; is the last one alternate?
+    int slot_rows[2], blocks[2], last_alt[2];  // rows of a slot; row blocks per kv head; is the last one alternate?
     int B, N, Hq, Hkv, G;
     int P, cap;                                // keys of the prefix; slots a sequence may have beyond it
     int early, grid;
@@ -104,7 +107,7 @@ template <typename F>
 __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const int* kv, F&& store) {
     int carry = p.Hkv * head_places(p, 0, steps_of(p.P));
 #pragma unroll
-    for (int i = 0; i < kMaxPrefixB / 32; ++i) {
+    for (int i = 0; i < kMaxLineB / 32; ++i) {
         if (i * 32 >= p.groups) break;
         const int b = i * 32 + lane;
         const int S = b < p.groups ? own_len(p, kv[i]) : -1;
@@ -200,6 +203,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
 }
 
 // (pa is not __grid_constant__: the producers hand a changed copy of it on, and with the attribute nvcc 12.9 passed the original)
+// ALONE: no sequence's own keys are on the line.  Then the two parts of a row that an alternate segment has are added up at its end,
+// because few_rows_kernel reads them for every sequence anew; otherwise they are two pieces (adding them up makes each tile wait for
+// the other, which costs the short segments of the sequences' own keys more than the pieces do: 60.9 -> 66.0 us for 8 trees of 60 nodes
+// of 32/32 heads, against 49.8 -> 46.5 us for 32 single tokens of 40/40 heads).
+template <bool ALONE>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PrefixParams p,
                    const PagedArgs pa) {
@@ -228,6 +236,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             mbar_init(bar(X_QWIDE + i), 129); mbar_init(bar(X_QALT + i), 32); mbar_init(bar(X_QEMPTY + i), 1);
             mbar_init(bar(X_OFULL + i), 1); mbar_init(bar(X_OFREE + i), 128);
         }
+        mbar_init(bar(X_STAT), 256);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -237,9 +246,9 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     }
     if (!p.early) pdl_wait();
     if (warp == 3) {
-        int kv[kMaxPrefixB / 32];
+        int kv[kMaxLineB / 32];
 #pragma unroll
-        for (int i = 0; i < kMaxPrefixB / 32; ++i) kv[i] = i * 32 + lane < p.groups ? p.kv_len[i * 32 + lane] : 0;
+        for (int i = 0; i < kMaxLineB / 32; ++i) kv[i] = i * 32 + lane < p.groups ? p.kv_len[i * 32 + lane] : 0;
         const int T = line_build(p, lane, kv, [&](int, int b, int at, int S) {
             if (b < p.groups) { sched.base[b + 1] = at; sched.len[b] = S; }
         });
@@ -318,7 +327,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         auto product = [&](int x, bool fresh, bool stage_done) {
             const uint32_t vb = v0 + sv * (STAGE >> 4);
             // (a segment's first PV product starts a fresh O: the last segment's must have been read)
-            if (fresh && seg > 0 && !wait(X_OFREE + x, (seg - 1) & 1)) return;
+            if (!ALONE && fresh && seg > 0 && !wait(X_OFREE + x, (seg - 1) & 1)) return;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (!wait(X_PFULL + 2 * x + h, (pp >> x) & 1)) return;
@@ -335,6 +344,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 if (++sv == NSV) { sv = 0; pv ^= 1; }
             }
         };
+        // (ALONE: by both tiles' threads, where it was an alternate segment)
+        auto o_free = [&]() { return !ALONE || seg == 0 || (wait(X_OFREE, (seg - 1) & 1) && wait(X_OFREE + 1, (seg - 1) & 1)); };
         // An alternate segment's next score, if it may be issued (wait_for_it: as soon as it may).
         auto alt_score = [&](int j, int n, bool wait_for_it) {
             auto have = [&](int i, uint32_t parity) {
@@ -355,10 +366,15 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 while (ok && scored < 2 && scored < n) scored += alt_score(scored, n, true);
                 fetch(n1, alt1);
                 for (int j = 0; j < n && ok; ++j) {
-                    if (!wait(X_VFULL + (int)sv, pv)) break;
+                    if (!wait(X_VFULL + (int)sv, pv) || (j == 0 && !o_free())) break;
                     product(px, j < 2, true);
                     if (!ok) break;
                     if (j + 2 >= n && leader) tc_commit(bar(X_OFULL + px));
+                    if (n == 1) {
+                        // (the tile without an operation keeps step as well: neither side may be two phases ahead of the other)
+                        if (!ALONE && seg > 0 && !wait(X_OFREE + (px ^ 1), (seg - 1) & 1)) break;
+                        if (leader) tc_commit(bar(X_OFULL + (px ^ 1)));
+                    }
                     px ^= 1;
                     // the tile's next score (overwrites P of this operation, which the product before it reads): of this segment, or of
                     // the next one where that is an alternate one (a wide one's Q rows come from threads that first have to end this
@@ -366,17 +382,13 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     if (scored < n) scored += alt_score(scored, n, true);
                     else if (alt1 && scored1 < n1) scored1 += alt_score(scored1, n1, false);
                 }
-                // (a tile without an operation keeps step as well: neither side may be two phases ahead of the other)
-                if (ok && n == 1) {
-                    if (seg == 0 || wait(X_OFREE + px, (seg - 1) & 1)) { if (leader) tc_commit(bar(X_OFULL + px)); }
-                }
             } else {
                 for (int x = 0; x < 2 && ok; ++x)
                     if (wait(X_QWIDE + x, qw) && (x == 1 || wait(X_KFULL + (int)sk, pk))) score(x, x, x == 1, n == 1);
                 qw ^= 1;
                 fetch(n1, alt1);
                 for (int t = 0; t < n && ok; ++t) {
-                    if (!wait(X_VFULL + (int)sv, pv)) break;
+                    if (!wait(X_VFULL + (int)sv, pv) || (t == 0 && !o_free())) break;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         if (!ok) break;
@@ -441,7 +453,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         PIter si = make_iter();
         PSeg sg;
         int it = 0, steps_before = 0, x0 = 0;                 // operations of this tile so far / steps of all segments so far / tile that begins
-        uint32_t o_phase = 0;
+        uint32_t o_phase = 0, stat_phase = 0;
         int fills[2] = {0, 0}, qr = 0;                        // how often each Q region has been filled; the next alternate segment's
         bool ok = true;
         // wide: Q tile -> shared memory, rows in the swizzled K-major layout of a K stage, asked for here and handed over by q_here.
@@ -606,36 +618,80 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             if (!ok) break;
             steps_before += sg.n;
-            const int piece = sg.alt ? x ^ x0 : x;                // (an alternate unit of one step has only the piece of the tile that began)
+            const int piece = sg.alt ? x ^ x0 : x;            // (an alternate segment of one step has only the piece of the tile that began)
             x0 = sg.alt ? x0 ^ (sg.n & 1) : 0;
 
             // ---- segment epilogue: the row's partial; the next segment's Q rows are asked for first ----
-            const int rows2 = 2 * p.half[sg.kind];
-            float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * rows2 + piece * (rows2 >> 1) + tl;
-            if (row_ok) p.part_ml[sg.kind][(size_t)sg.slot * rows2 + piece * (rows2 >> 1) + tl] = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
+            const bool alt = sg.alt;
+            const int rows = p.slot_rows[sg.kind];
+            const int at = ALONE ? tile0 + tl : piece * (rows >> 1) + tl;
+            float4* prow = p.part_o[sg.kind] + (size_t)sg.slot * (D / 4) * rows + at;
+            float2* pml = p.part_ml[sg.kind] + (size_t)sg.slot * rows + at;
             live = si.next(sg);
             if (live) q_ask();
             if (!ok || !(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
-            o_phase ^= 1;
-            tc_fence_after();
+            float2 ml = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
             // O is free for the next segment's products as soon as it has been read, ahead of the last stores.  (No partial is read before
             // this kernel has ended, so the arrival need not wait for them.)
-            if (warp_rows) {
+            if (ALONE && alt) {
+                // Both tiles have a part of every row; each adds up half of the columns.  (The statistics of the last alternate segment
+                // have been read by everybody: O is complete only after both tiles have let go of the last one's.)
+                if (!(ok = mbar_wait_warp(bar(X_OFULL + (x ^ 1)), o_phase, abort_flag))) break;
+                float2* stat = reinterpret_cast<float2*>(sm + SMEM_STAT);
+                stat[x * 128 + tl] = ml;
+                mbar_arrive(bar(X_STAT));
+                if (!(ok = mbar_wait_warp(bar(X_STAT), stat_phase, abort_flag))) break;
+                stat_phase ^= 1;
+                const float2 other = stat[(x ^ 1) * 128 + tl];
+                const float m = fmaxf(ml.x, other.x), m_use = m == -INFINITY ? 0.f : m;
+                const float w = exp2f(ml.x - m_use), u = exp2f(other.x - m_use);          // 0 for a tile that saw nothing
+                ml = make_float2(m, ml.y * w + other.y * u);
+                tc_fence_after();
+                if (warp_rows) {
+                    const uint32_t from = x * 64, peer = lane_addr + COL_O + (x ^ 1) * 128;
+                    prow += (size_t)(x * 16) * rows;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(o_addr + c * 32, o);
-                    tmem_wait_ld();
-                    if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
-                    if (row_ok && has_o) {                    // (without a product the piece has l = 0 and its o is not looked at)
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t o[32], q[32];
+                        tmem_ld32(o_addr + from + c * 32, o);
+                        tmem_ld32(peer + from + c * 32, q);
+                        tmem_wait_ld();
+                        if (c == 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
+                        if (row_ok) {
 #pragma unroll
-                        for (int c4 = 0; c4 < 8; ++c4, prow += rows2)
-                            *prow = make_float4(__uint_as_float(o[4 * c4]), __uint_as_float(o[4 * c4 + 1]), __uint_as_float(o[4 * c4 + 2]), __uint_as_float(o[4 * c4 + 3]));
+                            for (int c4 = 0; c4 < 8; ++c4, prow += rows) {
+                                float v[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)      // (undefined where no product ran)
+                                    v[e] = (w > 0.f ? w * __uint_as_float(o[4 * c4 + e]) : 0.f) + (u > 0.f ? u * __uint_as_float(q[4 * c4 + e]) : 0.f);
+                                *prow = make_float4(v[0], v[1], v[2], v[3]);
+                            }
+                        }
                     }
+                } else {
+                    mbar_arrive(bar(X_OFREE + x));
                 }
             } else {
-                mbar_arrive(bar(X_OFREE + x));
+                tc_fence_after();
+                if (warp_rows) {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(o_addr + c * 32, o);
+                        tmem_wait_ld();
+                        if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
+                        if (row_ok && has_o) {                // (without a product the piece has l = 0 and its o is not looked at)
+#pragma unroll
+                            for (int c4 = 0; c4 < 8; ++c4, prow += rows)
+                                *prow = make_float4(__uint_as_float(o[4 * c4]), __uint_as_float(o[4 * c4 + 1]), __uint_as_float(o[4 * c4 + 2]), __uint_as_float(o[4 * c4 + 3]));
+                        }
+                    }
+                } else {
+                    mbar_arrive(bar(X_OFREE + x));
+                }
             }
+            if (row_ok && (!(ALONE && alt) || x == 0)) *pml = ml;
+            o_phase ^= 1;
         }
     }
     tc_fence_before();
@@ -660,36 +716,34 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
     const long long li = live ? idx : all - 1;
     const int r = (int)(li % RG), cg = (int)(li / RG % CG), kvh = (int)(li / RG / CG % p.Hkv), b = (int)(li / RG / CG / p.Hkv);
     // the line, from kv_len, which the attention kernel does not write: every lane takes part in the sums, then takes its sequence's
-    int kv[kMaxPrefixB / 32], at[kMaxPrefixB / 32], own[kMaxPrefixB / 32];
+    int kv[kMaxLineB / 32], at[kMaxLineB / 32], own[kMaxLineB / 32];
     if (!p.early) pdl_wait();
 #pragma unroll
-    for (int i = 0; i < kMaxPrefixB / 32; ++i) { kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0; at[i] = 0; own[i] = -1; }
+    for (int i = 0; i < kMaxLineB / 32; ++i) { kv[i] = i * 32 + lane < p.B ? p.kv_len[i * 32 + lane] : 0; at[i] = 0; own[i] = -1; }
     const int T = line_build(p, lane, kv, [&](int i, int, int place, int S) { at[i] = place; own[i] = S; });
     int base_b = 0, S = -1;
 #pragma unroll
-    for (int i = 0; i < kMaxPrefixB / 32; ++i) {
+    for (int i = 0; i < kMaxLineB / 32; ++i) {
         const int x = __shfl_sync(0xffffffffu, at[i], b & 31), y = __shfl_sync(0xffffffffu, own[i], b & 31);
         if (b >> 5 == i) { base_b = x; S = y; }
     }
     const int R = range_of(T, p.grid);
     const int node = r / p.G, head = kvh * p.G + r % p.G;
-    // entry e of a kind: piece of CTA c0 + e (wide) or c0 + e / 2, tile e & 1 (alternate)
-    int c0[2], n[2], first[2];
-    bool alt[2];
+    int n[2], first[2];                                   // pieces of a kind, row of the first one in its region
+    bool two[2] = {false, false};                         // two pieces to a slot
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
         const int keys = kind ? S + p.N : p.P, steps = S < 0 ? 0 : steps_of(keys), row = kind ? r : b * RG + r;
-        const int m = row / kRows, lr = row - m * kRows, nb = p.blocks[kind], rows = min(kRows, (kind ? RG : p.B * RG) - m * kRows);
-        n[kind] = 0;
+        const int m = row / kRows, nb = p.blocks[kind];
+        n[kind] = first[kind] = 0;
         if (steps == 0) continue;
-        alt[kind] = rows <= 128;
-        const int u0 = (kind ? base_b : 0) + kvh * head_places(p, kind, steps) + m * unit_places(p, kind, steps, false) + start_places(alt[kind]);
-        c0[kind] = u0 / R;
-        const int c1 = (u0 + (steps - 1) * step_places(alt[kind])) / R;
-        n[kind] = (c1 - c0[kind] + 1) * (alt[kind] ? 2 : 1);
-        if (steps == 1) n[kind] = 1;                          // (an alternate unit of one step: the second tile has nothing)
-        const int unit = kind ? (b * p.Hkv + kvh) * nb + m : kvh * nb + m;
-        first[kind] = (unit + c0[kind]) * 2 * p.half[kind] + lr % 128 + (!alt[kind] && lr >= 128 ? p.half[kind] : 0);
+        const bool alt = m == nb - 1 && p.last_alt[kind];
+        const int u0 = (kind ? base_b : 0) + kvh * head_places(p, kind, steps) + m * unit_places(p, kind, steps, false) + start_places(alt);
+        const int c0 = u0 / R, unit = kind ? (b * p.Hkv + kvh) * nb + m : kvh * nb + m;
+        const int lr = row - m * kRows;
+        two[kind] = alt && steps > 1;                     // (an alternate unit of one step: the second tile has nothing)
+        n[kind] = ((u0 + (steps - 1) * step_places(alt)) / R - c0 + 1) << (two[kind] ? 1 : 0);
+        first[kind] = (unit + c0) * p.slot_rows[kind] + (lr < 128 ? lr : (p.slot_rows[kind] >> 1) + lr - 128);
     }
     if (p.early) pdl_wait();
     if (!live) return;
@@ -709,14 +763,14 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
 #pragma unroll
             for (int k = 0; k < C4; ++k) v[u][k] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (e < entries) {
-                const int kind = e < n[0] ? 0 : 1, ek = kind ? e - n[0] : e, half = kind ? p.half[1] : p.half[0];
-                const bool a = kind ? alt[1] : alt[0];
-                const int pos = (kind ? first[1] : first[0]) + (a ? (ek >> 1) * 2 * half + (ek & 1) * half : ek * 2 * half);   // row of the region
-                const int slot = pos / (2 * half), in = pos - slot * 2 * half;
-                ml[u] = __ldcg((kind ? p.part_ml[1] : p.part_ml[0]) + pos);
-                const float4* src = (kind ? p.part_o[1] : p.part_o[0]) + ((size_t)slot * (D / 4) + cg * C4) * 2 * half + in;
+                const bool own = e >= n[0];
+                const int rows = own ? p.slot_rows[1] : p.slot_rows[0], ek = own ? e - n[0] : e;
+                const int pos = (own ? first[1] : first[0]) + ((own ? two[1] : two[0]) ? ek * (rows >> 1) : ek * rows);
+                const int slot = pos / rows, in = pos - slot * rows;
+                ml[u] = __ldcg((own ? p.part_ml[1] : p.part_ml[0]) + pos);
+                const float4* src = (own ? p.part_o[1] : p.part_o[0]) + ((size_t)slot * (D / 4) + cg * C4) * rows + in;
 #pragma unroll
-                for (int k = 0; k < C4; ++k) v[u][k] = __ldcg(src + (size_t)k * 2 * half);
+                for (int k = 0; k < C4; ++k) v[u][k] = __ldcg(src + (size_t)k * rows);
             }
         }
         float m_new = m_all;
@@ -948,25 +1002,25 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
     // ---- the prefix's pieces of these rows, from the kernel before ----
     if (p.early && p.P > 0) pdl_wait();
     if (good && live && p.P > 0) {
-        const int steps = steps_of(p.P), Rg = range_of(p.Hkv * head_places(p, 0, steps), p.grid), rows2 = 2 * p.half[0];
+        const int steps = steps_of(p.P), Rg = range_of(p.Hkv * head_places(p, 0, steps), p.grid), rows = p.slot_rows[0];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int row = b * RG + min(c8 + 8 * r, RG - 1), m = row / kRows, lr = row - m * kRows, nb = p.blocks[0];
-            const bool alt = min(kRows, p.B * RG - m * kRows) <= 128;
+            const bool alt = m == nb - 1 && p.last_alt[0];
             const int u0 = kvh * head_places(p, 0, steps) + m * unit_places(p, 0, steps, false) + start_places(alt);
             const int first = u0 / Rg, last = (u0 + (steps - 1) * step_places(alt)) / Rg;
-            const int pieces = (last - first + 1) * (alt ? 2 : 1);
+            const int pieces = last - first + 1;
             for (int e0 = wi; e0 < pieces; e0 += 2 * nw) {                                   // two at a time, their loads ahead of the sums
                 float2 ml[2];
                 float4 v[2][8];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int e = e0 + k * nw < pieces ? e0 + k * nw : e0;
-                    const int slot = kvh * nb + m + first + (alt ? e >> 1 : e), in = alt ? (e & 1) * p.half[0] + lr : lr;
-                    ml[k] = __ldcg(p.part_ml[0] + (size_t)slot * rows2 + in);
-                    const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows2 + in;
+                    const int slot = kvh * nb + m + first + e;
+                    ml[k] = __ldcg(p.part_ml[0] + (size_t)slot * rows + lr);
+                    const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows + lr;
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows2);
+                    for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows);
                 }
                 if (e0 + nw >= pieces) ml[1] = make_float2(-INFINITY, 0.f);
 #pragma unroll
@@ -1043,19 +1097,21 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
 
 // What of the scratch a call of B sequences of N nodes uses.
 struct PrefixLayout {
-    int rows[2], blocks[2], half[2];
+    int rows[2], blocks[2], slot_rows[2];
     long long slots[2];
     size_t bytes[2];
 };
 PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count) {
     PrefixLayout l;
+    const bool alone = N * (Hq / Hkv) <= kFewRows;
     const int G = Hq / Hkv;
     for (int kind = 0; kind < 2; ++kind) {
         l.rows[kind] = (kind ? N : B * N) * G;
         l.blocks[kind] = (l.rows[kind] + kRows - 1) / kRows;
-        l.half[kind] = l.rows[kind] > 128 ? 128 : (l.rows[kind] + 7) / 8 * 8;
+        const int rows8 = (l.rows[kind] + 7) / 8 * 8;
+        l.slot_rows[kind] = l.rows[kind] > 128 ? (alone && rows8 < kRows ? rows8 : kRows) : alone ? rows8 : 2 * rows8;
         l.slots[kind] = (long long)(kind ? B : 1) * Hkv * l.blocks[kind] + sm_count;
-        l.bytes[kind] = (size_t)l.slots[kind] * 2 * l.half[kind] * (D * 4 + 8);
+        l.bytes[kind] = (size_t)l.slots[kind] * l.slot_rows[kind] * (D * 4 + 8);
     }
     return l;
 }
@@ -1078,18 +1134,20 @@ cudaError_t init_attn_prefix() {
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(r));
         if (e != cudaSuccess) return e;
     }
-    return cudaFuncSetAttribute((const void*)attn_prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)attn_prefix_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute((const void*)attn_prefix_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
 }
 
 // Sizes that these kernels take: every place of the line and every row of the partials has a 32-bit number.
 bool attn_prefix_supports(const AttnArgs& a, int prefix) {
-    if (a.B > kMaxPrefixB || !(a.scale > 0.f) || a.D != D || !a.page_rows) return false;
+    const bool few = a.N * (a.Hq / a.Hkv) <= kFewRows;
+    if ((!few && a.B > kMaxLineB) || !(a.scale > 0.f) || a.D != D || !a.page_rows) return false;
     const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
     long long T = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const long long steps = ((kind ? (long long)a.S_max - prefix : prefix) + STEP - 1) / STEP;
         T += (kind ? (long long)a.B : 1) * a.Hkv * l.blocks[kind] * (kWideStart + steps * kWideStep);
-        if (l.slots[kind] * 2 * l.half[kind] >= (1ll << 31)) return false;
+        if (l.slots[kind] * l.slot_rows[kind] >= (1ll << 31)) return false;
     }
     return T < (1ll << 31) - (1 << 20);
 }
@@ -1102,11 +1160,11 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
     unsigned char* ws = (unsigned char*)scratch;
     for (int kind = 0; kind < 2; ++kind) {
         p.part_o[kind] = (float4*)ws;
-        ws += (size_t)l.slots[kind] * 2 * l.half[kind] * D * 4;
-        p.half[kind] = l.half[kind]; p.blocks[kind] = l.blocks[kind];
+        ws += (size_t)l.slots[kind] * l.slot_rows[kind] * D * 4;
+        p.slot_rows[kind] = l.slot_rows[kind]; p.blocks[kind] = l.blocks[kind];
         p.last_alt[kind] = l.rows[kind] - (l.blocks[kind] - 1) * kRows <= 128;
     }
-    for (int kind = 0; kind < 2; ++kind) { p.part_ml[kind] = (float2*)ws; ws += (size_t)l.slots[kind] * 2 * l.half[kind] * 8; }
+    for (int kind = 0; kind < 2; ++kind) { p.part_ml[kind] = (float2*)ws; ws += (size_t)l.slots[kind] * l.slot_rows[kind] * 8; }
     p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv;
     p.P = prefix; p.cap = a.S_max - prefix;
     p.early = a.early_prefetch ? 1 : 0; p.grid = a.sm_count; p.groups = a.B;
@@ -1117,7 +1175,8 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
     if (few) p.groups = 0;
     cudaError_t err = cudaSuccess;
     if (!few || prefix > 0) {
-        err = launch_pdl(attn_prefix_kernel, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa);
+        err = few ? launch_pdl(attn_prefix_kernel<true>, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa)
+                  : launch_pdl(attn_prefix_kernel<false>, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa);
         if (err != cudaSuccess) return err;
         ++*n_launches;
     }
@@ -1125,7 +1184,7 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         // Warps to a unit: as many as the SMs hold at once, as long as each has a group of keys
         // or a piece of the prefix.
         const int units = a.B * a.Hkv, steps = steps_of(prefix), T = a.Hkv * head_places(p, 0, steps);
-        const int pieces = steps == 0 ? 0 : 2 * unit_places(p, 0, steps, true) / range_of(T, p.grid) + 1, most = std::max((p.cap + 15) / 16, pieces);
+        const int pieces = steps == 0 ? 0 : unit_places(p, 0, steps, true) / range_of(T, p.grid) + 1, most = std::max((p.cap + 15) / 16, pieces);
         const int room = (l.rows[1] <= 8 ? 12 : 8) * a.sm_count;
         int nw = 1;
         while (nw < 8 * kFewWarps && 2 * nw <= most && units * 2 * nw <= room) nw *= 2;

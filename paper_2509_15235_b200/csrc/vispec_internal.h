@@ -135,7 +135,6 @@ cudaError_t init_attn_tc5_wide();
 WidePlan attn_tc5_wide_plan(const AttnArgs& a);
 cudaError_t launch_attn_tc5_wide(const AttnArgs& a, const WidePlan& w, cudaStream_t st, int* n_launches);
 // Attention over a prefix that all sequences share, then their own keys (attn_prefix.cu); a.S_max: slots of a table row.
-constexpr int kMaxPrefixB = 128;                  // sequences per call
 size_t prefix_scratch_bytes(int B, int N, int Hq, int Hkv, int sm_count);
 cudaError_t init_attn_prefix();
 bool attn_prefix_supports(const AttnArgs& a, int prefix);

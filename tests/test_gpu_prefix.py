@@ -112,6 +112,10 @@ CASES = {
     "tree_129_rows": (3, 43, 3, 1, 300, [7, 140, 2]),             # own 129 rows: one row in the second tile
     "nothing_shared": (3, 20, 4, 2, 0, [300, 0, 129]),
     "many": (128, 1, 4, 2, 512, [0, 3, 40, 200]),
+    "hundreds": (300, 1, 7, 1, 272, [0, 3, 40, 130, 77]),         # prefix rows in nine blocks
+    "few_16_rows": (5, 4, 8, 2, 160, [0, 300, 40, 7, 1000]),      # 16 rows per sequence and kv head
+    "few_rows_blocks": (9, 8, 8, 4, 2000, [5, 0, 333]),           # 16 rows, prefix of 144: 128 and 16
+    "just_above_few": (3, 17, 2, 2, 500, [5, 200, 64]),
     "many_trees": (40, 8, 8, 8, 256, [10, 60, 0, 300, 5]),
     "long_own": (2, 4, 4, 1, 96, [4000, 2500]),
 }
@@ -435,13 +439,19 @@ def test_refusals():
     assert lib.vispec_tree_verify_attn_prefix_paged(z, 0, z, z, z, 1, 0, z, 1, 1, 1.0, z, 0, z, z, z) == E_NULL
     assert ctx.status_poll() == 0
     ctx.close()
-    big = b.VerifyContext(129, 1, 2, 2, 128, 128, 1)
+    # more than 16 rows per sequence and kv head: at most 64 sequences
+    big = b.VerifyContext(65, 9, 4, 2, 128, 128, 1)
     pool = torch.zeros((8, 2, 16, 128), dtype=torch.bfloat16, device="cuda")
     big.cache_register_paged(0, pool, pool)
-    q = torch.zeros((129, 1, 2, 128), dtype=torch.bfloat16, device="cuda")
-    with pytest.raises(b.VispecError) as e:
-        big.tree_verify_attn_prefix_paged(0, q, torch.zeros(129, dtype=torch.int32, device="cuda"),
-                                          torch.zeros((129, 8), dtype=torch.int32, device="cuda"), 0,
-                                          torch.ones((129, 1, 1), dtype=torch.int64, device="cuda"), SCALE, big.prefix_scratch(129, 1), q)
-    assert e.value.code == E_UNSUP
+    for N, fine in ((9, False), (8, True)):
+        q = torch.zeros((65, N, 4, 128), dtype=torch.bfloat16, device="cuda")
+        args = (0, q, torch.zeros(65, dtype=torch.int32, device="cuda"), torch.zeros((65, 8), dtype=torch.int32, device="cuda"), 0,
+                torch.ones((65, N, 1), dtype=torch.int64, device="cuda"), SCALE, big.prefix_scratch(65, N), q.clone())
+        if fine:
+            big.tree_verify_attn_prefix_paged(*args)
+        else:
+            with pytest.raises(b.VispecError) as e:
+                big.tree_verify_attn_prefix_paged(*args)
+            assert e.value.code == E_UNSUP
+    assert big.status_poll() == 0
     big.close()
