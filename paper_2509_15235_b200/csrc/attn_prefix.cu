@@ -79,6 +79,7 @@ struct PrefixParams {
     int B, N, Hq, Hkv, G;
     int P, cap;                                // keys of the prefix; slots a sequence may have beyond it
     int early, grid;
+    int pad, range;                            // prefix alone on a line shorter than the SMs: places of a unit, and of a CTA (0: see range_of)
     int groups;                                // sequences whose own keys are on the line: B, or 0 where few_rows_kernel takes them
     float scale_log2;
     int* status;
@@ -86,11 +87,12 @@ struct PrefixParams {
 
 // Places of the line (some 210 cycles each, from clock stamps of 8 x 60 nodes of 32/32 heads): a wide step 3400 cycles, an alternate
 // one 1900, the start of a segment (Q rows, first score, last product, partials) 7500 and 3500.
-constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 36;
+constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 32;
 __host__ __device__ constexpr int step_places(bool alt) { return alt ? kAltStep : kWideStep; }
 __host__ __device__ constexpr int start_places(bool alt) { return alt ? kAltStart : kWideStart; }
 
 __host__ __device__ __forceinline__ int unit_places(const PrefixParams& p, int kind, int steps, bool last) {
+    if (kind == 0 && p.pad) return p.pad;
     const bool alt = last && p.last_alt[kind];
     return start_places(alt) + steps * step_places(alt);
 }
@@ -123,7 +125,10 @@ __device__ __forceinline__ int line_build(const PrefixParams& p, int lane, const
     }
     return carry;
 }
-__host__ __device__ __forceinline__ int range_of(int T, int grid) { return (T + grid - 1) / grid > kMinRange ? (T + grid - 1) / grid : kMinRange; }
+__host__ __device__ __forceinline__ int range_of(const PrefixParams& p, int T) {
+    const int even = (T + p.grid - 1) / p.grid;
+    return p.range ? p.range : even > kMinRange ? even : kMinRange;
+}
 
 // The first step of a unit that starts at `start` whose place is at or behind g.
 __device__ __forceinline__ int step_at(int g, int start, bool alt) {
@@ -252,7 +257,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const int T = line_build(p, lane, kv, [&](int, int b, int at, int S) {
             if (b < p.groups) { sched.base[b + 1] = at; sched.len[b] = S; }
         });
-        if (lane == 0) { sched.base[0] = 0; sched.base[p.groups + 1] = T; sched.range = range_of(T, p.grid); }
+        if (lane == 0) { sched.base[0] = 0; sched.base[p.groups + 1] = T; sched.range = range_of(p, T); }
     }
     tc_fence_before();
     __syncthreads();
@@ -727,7 +732,7 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
         const int x = __shfl_sync(0xffffffffu, at[i], b & 31), y = __shfl_sync(0xffffffffu, own[i], b & 31);
         if (b >> 5 == i) { base_b = x; S = y; }
     }
-    const int R = range_of(T, p.grid);
+    const int R = range_of(p, T);
     const int node = r / p.G, head = kvh * p.G + r % p.G;
     int n[2], first[2];                                   // pieces of a kind, row of the first one in its region
     bool two[2] = {false, false};                         // two pieces to a slot
@@ -1002,7 +1007,7 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
     // ---- the prefix's pieces of these rows, from the kernel before ----
     if (p.early && p.P > 0) pdl_wait();
     if (good && live && p.P > 0) {
-        const int steps = steps_of(p.P), Rg = range_of(p.Hkv * head_places(p, 0, steps), p.grid), rows = p.slot_rows[0];
+        const int steps = steps_of(p.P), Rg = range_of(p, p.Hkv * head_places(p, 0, steps)), rows = p.slot_rows[0];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int row = b * RG + min(c8 + 8 * r, RG - 1), m = row / kRows, lr = row - m * kRows, nb = p.blocks[0];
@@ -1172,7 +1177,17 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
     p.status = a.status;
     const PagedArgs pa = {a.block_table, a.table_stride, a.page_rows, a.num_blocks, a.Hkv, a.N, a.token_major, a.status, nullptr};
     const bool few = l.rows[1] <= kFewRows;
-    if (few) p.groups = 0;
+    if (few) {
+        p.groups = 0;
+        // More SMs than ranges worth having: a unit is cut into equal parts of whole ranges, so that no CTA starts on a second unit
+        // while others have none.
+        const int steps = steps_of(prefix), n = a.Hkv * l.blocks[0], len = unit_places(p, 0, steps, l.blocks[0] == 1);
+        if (steps > 0 && n <= a.sm_count && a.Hkv * head_places(p, 0, steps) < a.sm_count * kMinRange) {
+            const int parts = std::max(1, std::min(a.sm_count / n, len / kMinRange));
+            p.range = (len + parts - 1) / parts;
+            p.pad = parts * p.range;
+        }
+    }
     cudaError_t err = cudaSuccess;
     if (!few || prefix > 0) {
         err = few ? launch_pdl(attn_prefix_kernel<true>, dim3(p.grid), dim3(kThreads), SMEM_ALLOC, st, 0, *a.k_map, *a.v_map, p, pa)
@@ -1184,7 +1199,7 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         // Warps to a unit: as many as the SMs hold at once, as long as each has a group of keys
         // or a piece of the prefix.
         const int units = a.B * a.Hkv, steps = steps_of(prefix), T = a.Hkv * head_places(p, 0, steps);
-        const int pieces = steps == 0 ? 0 : unit_places(p, 0, steps, true) / range_of(T, p.grid) + 1, most = std::max((p.cap + 15) / 16, pieces);
+        const int pieces = steps == 0 ? 0 : unit_places(p, 0, steps, true) / range_of(p, T) + 1, most = std::max((p.cap + 15) / 16, pieces);
         const int room = (l.rows[1] <= 8 ? 12 : 8) * a.sm_count;
         int nw = 1;
         while (nw < 8 * kFewWarps && 2 * nw <= most && units * 2 * nw <= room) nw *= 2;
