@@ -363,7 +363,7 @@ int vispec_rope_axes_rows(vispec_ctx* ctx, const void* q, int64_t q_stride, cons
  * its q_out rows included, with status word VISPEC_E_RANGE; a cu_len that decreases, starts below 0 or ends beyond T drops
  * the whole call, with the same code.  All other slots keep their bytes.  One launch.  The call writes committed slots and kv_len_out:
  * for the attention calls after it the rule of VISPEC_OPT_EARLY_PREFETCH applies as for a commit.
- * Host errors: E_NULL, E_ALIGN, E_SHAPE (B outside [0, B_max] or above 8192, T < 0, strides, axes), E_RANGE (layer),
+ * Host errors: E_NULL, E_ALIGN, E_SHAPE (B outside [0, B_max] or above 4096, T < 0, strides, axes), E_RANGE (layer),
  * E_UNREGISTERED, E_UNSUPPORTED (paged layer), E_CUDA. */
 int vispec_kv_append(vispec_ctx* ctx, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
                      const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes /*host*/,

@@ -82,7 +82,7 @@ struct RowsArgs {
     int B, S_max;
     int* status;
 };
-constexpr int kMaxAppendB = 8192;              // sequences per append: their ends sit in shared memory
+constexpr int kMaxAppendB = 4096;              // sequences per append: their ends and lengths sit in shared memory
 cudaError_t launch_prompt_rows(const RowsArgs& a, bool append, int D, int sm_count, cudaStream_t st,
                                const int32_t* block_table = nullptr, int table_stride = 0, int page_rows = 0,
                                int num_blocks = 0, int token_major = 0);
