@@ -282,7 +282,7 @@ int vispec_tree_verify_attn_paged(vispec_ctx* ctx, int layer, const void* q, con
  * kv_len[b] counts the prefix too; a sequence with kv_len[b] below the shared slots or kv_len[b] + N above the table's
  * capacity gets out = 0, lse = -inf and the status word VISPEC_E_RANGE.  No workspace is used.  At most 64 sequences where
  * N * Hq / Hkv > 16; any number up to B_max otherwise.
- * Host errors: E_NULL, E_ALIGN, E_SHAPE, E_RANGE (layer, prefix_len), E_UNREGISTERED, E_UNSUPPORTED (contiguous layer,
+ * Host errors: E_NULL, E_ALIGN, E_SHAPE, E_RANGE (layer, prefix_len, device), E_UNREGISTERED, E_UNSUPPORTED (contiguous layer,
  * too many sequences, scale <= 0, sizes beyond 2^31 schedule places), E_WORKSPACE (scratch too small), E_CUDA. */
 int vispec_tree_verify_attn_prefix_paged(vispec_ctx* ctx, int layer, const void* q, const int32_t* kv_len,
                                          const int32_t* block_table, int table_stride, int prefix_len /*host*/,
@@ -346,7 +346,7 @@ typedef struct vispec_rope_axes {
  * or k with k_out, may be NULL: those rows are not processed.  Angles are reduced in fp64, sines and products are fp32, one
  * rounding to bf16.  T = 0 does nothing.
  * Host errors: E_NULL (also both pairs NULL, one half of a pair NULL), E_ALIGN (pointers 16 B, strides multiples of 8),
- * E_SHAPE (T < 0, a stride below the row, theta <= 1, sections that do not fit D/2, in place with another stride), E_CUDA. */
+ * E_RANGE (the context's device is not the current one), E_SHAPE (T < 0, a stride below the row, theta <= 1, sections that do not fit D/2, in place with another stride), E_CUDA. */
 int vispec_rope_axes_rows(vispec_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                           const int32_t* positions, int T, const vispec_rope_axes* axes /*host*/, void* q_out,
                           int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
@@ -363,15 +363,15 @@ int vispec_rope_axes_rows(vispec_ctx* ctx, const void* q, int64_t q_stride, cons
  * its q_out rows included, with status word VISPEC_E_RANGE; a cu_len that decreases, starts below 0 or ends beyond T drops
  * the whole call, with the same code.  All other slots keep their bytes.  One launch.  The call writes committed slots and kv_len_out:
  * for the attention calls after it the rule of VISPEC_OPT_EARLY_PREFETCH applies as for a commit.
- * Host errors: E_NULL, E_ALIGN, E_SHAPE (B outside [0, B_max] or above 4096, T < 0, strides, axes), E_RANGE (layer),
+ * Host errors: E_NULL, E_ALIGN, E_SHAPE (B outside [0, B_max] or above 4096, T < 0, strides, axes), E_RANGE (layer, device),
  * E_UNREGISTERED, E_UNSUPPORTED (paged layer), E_CUDA. */
 int vispec_kv_append(vispec_ctx* ctx, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
                      const void* v_new, int64_t v_stride, const int32_t* positions, const vispec_rope_axes* axes /*host*/,
                      const int32_t* cu_len, const int32_t* kv_len, int B, int T, void* q_out, int64_t q_out_stride,
                      int32_t* kv_len_out, void* stream);
 /* The same on a paged layer: slots are found through block_table [B,table_stride] (capacity table_stride * page_rows); a
- * table entry outside the pool drops that row's k and v and sets the status word VISPEC_E_RANGE.  E_UNSUPPORTED for a
- * contiguous layer. */
+ * table entry outside the pool drops that row's k and v and sets the status word VISPEC_E_RANGE.  A block that several
+ * sequences share (a prefix) is written through one of them only.  E_UNSUPPORTED for a contiguous layer. */
 int vispec_kv_append_paged(vispec_ctx* ctx, int layer, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
                            const void* v_new, int64_t v_stride, const int32_t* positions,
                            const vispec_rope_axes* axes /*host*/, const int32_t* cu_len, const int32_t* kv_len,

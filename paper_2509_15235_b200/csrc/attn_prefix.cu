@@ -187,7 +187,7 @@ struct PIter {
             o.n = steps;
             start += m == nb - 1 ? last : full;
             if (here < lo) o.st0 = step_at(lo, here, o.alt);
-            if (start > hi) o.n = step_at(hi, here, o.alt);        // (at most the unit's steps)
+            if (start > hi) o.n = min(steps, step_at(hi, here, o.alt));     // (a padded unit ends behind its last step)
             o.n -= o.st0;
             if (++m == nb) {
                 m = 0;
@@ -1115,7 +1115,7 @@ PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count) {
         l.blocks[kind] = (l.rows[kind] + kRows - 1) / kRows;
         const int rows8 = (l.rows[kind] + 7) / 8 * 8;
         l.slot_rows[kind] = l.rows[kind] > 128 ? (alone && rows8 < kRows ? rows8 : kRows) : alone ? rows8 : 2 * rows8;
-        l.slots[kind] = (long long)(kind ? B : 1) * Hkv * l.blocks[kind] + sm_count;
+        l.slots[kind] = kind && alone ? 0 : (long long)(kind ? B : 1) * Hkv * l.blocks[kind] + sm_count;     // (few_rows_kernel parks nothing)
         l.bytes[kind] = (size_t)l.slots[kind] * l.slot_rows[kind] * (D * 4 + 8);
     }
     return l;
@@ -1149,7 +1149,7 @@ bool attn_prefix_supports(const AttnArgs& a, int prefix) {
     if ((!few && a.B > kMaxLineB) || !(a.scale > 0.f) || a.D != D || !a.page_rows) return false;
     const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
     long long T = 0;
-    for (int kind = 0; kind < 2; ++kind) {
+    for (int kind = 0; kind < (few ? 1 : 2); ++kind) {
         const long long steps = ((kind ? (long long)a.S_max - prefix : prefix) + STEP - 1) / STEP;
         T += (kind ? (long long)a.B : 1) * a.Hkv * l.blocks[kind] * (kWideStart + steps * kWideStep);
         if (l.slots[kind] * l.slot_rows[kind] >= (1ll << 31)) return false;

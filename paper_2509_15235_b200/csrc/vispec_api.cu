@@ -396,6 +396,12 @@ int vispec_tree_verify_attn_paged(vispec_ctx* c, int layer, const void* q, const
     return err == cudaSuccess ? VISPEC_OK : VISPEC_E_CUDA;
 }
 
+// The context's device is the current one (its memory and the kernels' attributes belong to it).
+static bool on_device(const vispec_ctx* c) {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
 int vispec_prefix_scratch_bytes(const vispec_ctx* c, int B, int N, size_t* out) {
     if (!c || !out) return VISPEC_E_NULL;
     if (B < 0 || B > c->shape.B_max || N < 1 || N > c->shape.N_max) return VISPEC_E_SHAPE;
@@ -419,6 +425,7 @@ int vispec_tree_verify_attn_prefix_paged(vispec_ctx* c, int layer, const void* q
     if ((long long)table_stride * pr > (1ll << 30)) return VISPEC_E_SHAPE;
     if (prefix_len < 0 || prefix_len > table_stride * pr) return VISPEC_E_RANGE;
     if (B == 0) return VISPEC_OK;
+    if (!on_device(c)) return VISPEC_E_RANGE;
     AttnArgs a = {};
     a.q = q; a.k = c->h_k[layer]; a.v = c->h_v[layer];
     a.kv_len = kv_len; a.mask = tree_mask; a.out = out; a.lse = lse;
@@ -567,6 +574,7 @@ int vispec_rope_axes_rows(vispec_ctx* c, const void* q, int64_t q_stride, const 
     RowsArgs a = {};
     if (T < 0 || !set_axes(a, axes, s.D)) return VISPEC_E_SHAPE;
     if (T == 0) return VISPEC_OK;
+    if (!on_device(c)) return VISPEC_E_RANGE;
     if (!positions || (!q && !k) || !q != !q_out || !k != !k_out) return VISPEC_E_NULL;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || (q && ((q_stride | q_out_stride) & 7)) ||
         (k && ((k_stride | k_out_stride) & 7)))
@@ -592,6 +600,7 @@ static int append_rows(vispec_ctx* c, int layer, const void* q, int64_t q_stride
     RowsArgs a = {};
     if (axes && !set_axes(a, axes, s.D)) return VISPEC_E_SHAPE;
     if (B == 0) return VISPEC_OK;
+    if (!on_device(c)) return VISPEC_E_RANGE;
     if (T > 0) {
         if (!k_new || !v_new || !q != !q_out || (axes && !positions)) return VISPEC_E_NULL;
         if (!axes && (q || positions)) return VISPEC_E_SHAPE;

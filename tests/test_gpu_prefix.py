@@ -115,6 +115,9 @@ CASES = {
     "hundreds": (300, 1, 7, 1, 272, [0, 3, 40, 130, 77]),         # prefix rows in nine blocks
     "few_16_rows": (5, 4, 8, 2, 160, [0, 300, 40, 7, 1000]),      # 16 rows per sequence and kv head
     "few_rows_blocks": (9, 8, 8, 4, 2000, [5, 0, 333]),           # 16 rows, prefix of 144: 128 and 16
+    # prefix of 560 rows, two blocks of 256 and one of 48 in alternate steps, each cut into as many parts as a whole block
+    "few_short_last_block": (40, 2, 28, 4, 2000, [300, 5, 0]),
+    "few_wide_last_block": (20, 5, 9, 3, 1500, [30, 5, 0]),       # 300 rows: 256 and 44
     "just_above_few": (3, 17, 2, 2, 500, [5, 200, 64]),
     "many_trees": (40, 8, 8, 8, 256, [10, 60, 0, 300, 5]),
     "long_own": (2, 4, 4, 1, 96, [4000, 2500]),
