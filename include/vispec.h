@@ -281,7 +281,7 @@ int vispec_tree_verify_attn_paged(vispec_ctx* ctx, int layer, const void* q, con
  *                nothing in it has to be cleared or kept.  Calls that may overlap on the GPU need scratch of their own.
  * kv_len[b] counts the prefix too; a sequence with kv_len[b] below the shared slots or kv_len[b] + N above the table's
  * capacity gets out = 0, lse = -inf and the status word VISPEC_E_RANGE.  No workspace is used.  At most 64 sequences where
- * N * Hq / Hkv > 16; any number up to B_max otherwise.
+ * N * Hq / Hkv > 8; any number up to B_max otherwise.
  * Host errors: E_NULL, E_ALIGN, E_SHAPE, E_RANGE (layer, prefix_len, device), E_UNREGISTERED, E_UNSUPPORTED (contiguous layer,
  * too many sequences, scale <= 0, sizes beyond 2^31 schedule places), E_WORKSPACE (scratch too small), E_CUDA. */
 int vispec_tree_verify_attn_prefix_paged(vispec_ctx* ctx, int layer, const void* q, const int32_t* kv_len,

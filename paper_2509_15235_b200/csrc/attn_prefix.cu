@@ -813,11 +813,11 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Few rows per unit (N * G <= 16: single tokens, small trees): the sequences' own keys, and the join with the prefix.
+// Few rows per unit (N * G <= 8: single tokens, small trees): the sequences' own keys, and the join with the prefix.
 //
 // What bounds it: the read of the own keys.  A tile of 128 rows would be nearly empty and its segments would cost more to start than
 // to stream (32 sequences x 40 heads with one row each: 8 segments per SM of 8 to 10 thousand cycles), so here a warp takes 16 keys at
-// a time on its own, by asynchronous 16-byte copies two or three groups deep into shared memory of its own, and has nothing to set up:
+// a time on its own, by asynchronous 16-byte copies into shared memory of its own, a group ahead, and has nothing to set up:
 //   S = Q K^T   (mma.sync m16n8k16) lane (key k = lane / 4, part q = lane % 4) reads 16 bytes of key k at elements 32 j + 8 q: the pairs
 //               are the B operand of two products whose 16 contracted elements are 32 j + 8 q' + 4 s + {0, 1} and + {2, 3}; Q alike.
 //   O += P V    P is S's accumulator layout read as an A operand.  The lane reads 16 bytes of keys 2q, 2q + 1, 2q + 8, 2q + 9 at
@@ -827,23 +827,21 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
 // A unit is a warp's, or that of 2 or 4 warps of a block, or where units are few of a cluster of 2, 4 or 8 blocks; they take the groups
 // of 16 keys and the prefix's pieces in turn, their (m, l, o) meet in shared memory and the row is finished here.
 // ------------------------------------------------------------------------------------------------
-constexpr int kFewWarps = 4, kFewRows = 16;
+constexpr int kFewWarps = 4, kFewRows = 8, kFewStages = 2;
 constexpr int kFewStage = 2 * 16 * D * 2;          // bytes of 16 keys and their values
-// Blocks of eight rows -> stages of a warp, blocks on an SM: the registers decide.
-__host__ __device__ constexpr int few_stages(int r) { return r == 1 ? 2 : 3; }
-__host__ __device__ constexpr int few_smem(int r) { return kFewWarps * few_stages(r) * kFewStage; }
+constexpr int kFewSmem = kFewWarps * kFewStages * kFewStage;
 
 __device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// R: blocks of 8 rows that exist (1 or 2).
-template <int R>
-__global__ void __launch_bounds__(32 * kFewWarps, R == 1 ? 3 : 2)
+// (Units of 9 to 16 rows the same way, two accumulators a lane and the registers of two blocks per SM, were no faster than on the line:
+// 16 x 2 nodes of 16/2 heads on 3000 + 1000 keys 25.9 us against 18.1, 24 x 16 of 32/32 on 2000 + 1500 131 against 109.)
+__global__ void __launch_bounds__(32 * kFewWarps, 3)
 few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ PagedArgs pa, const uint4* __restrict__ k_pool,
                 const uint4* __restrict__ v_pool, const int wpu /* warps of a block that share a unit */) {
-    constexpr int ROWS = 8 * R, kFewStages = few_stages(R);
+    constexpr int ROWS = 8;
     extern __shared__ __align__(1024) unsigned char sm[];
     __shared__ float2 park_ml[kFewWarps][ROWS];
     static_assert(ROWS * (D / 4 + 1) * 16 <= kFewStages * kFewStage, "a warp's part does not fit its stages");
@@ -854,41 +852,29 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
     const bool live = unit_ < units;               // (the last block may have warps without a unit)
     const int unit = live ? unit_ : units - 1, b = unit / p.Hkv, kvh = unit - b * p.Hkv;
     const int wi = ck > 1 ? cr * kFewWarps + warp : sub, nw = ck > 1 ? ck * kFewWarps : wpu;
-    const int RG = p.N * p.G, W = (p.N + 63) >> 6;
+    const int RG = p.N * p.G;
     if (!p.early) pdl_wait();
     pdl_launch_dependents();
     const int S = own_len(p, p.kv_len[b]), total = S + p.N;
     const bool good = S >= 0;
-    // Rows of this lane: c8 and, with R == 2, c8 + 8.  (q, tree_mask and the tree's own keys: the kernel before has waited for what
+    // The lane's row is c8.  (q, tree_mask and the tree's own keys: the kernel before has waited for what
     // writes them before it let this one in; where there is none, this one waits.)
     if (p.early && p.P == 0) pdl_wait();
-    uint32_t qa[D / 16][2 * R];                    // [j * 2 + s]: A registers (row, row + 8) x (first, second half of the 16 elements)
-    uint64_t mk[R][2];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int row = c8 + 8 * r;
-        const bool there = row < RG;
-        const int node = there ? row / p.G : 0, head = kvh * p.G + (there ? row % p.G : 0);
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (((size_t)b * p.N + node) * p.Hq + head) * D) + q4;
+    const bool there = c8 < RG;
+    const int node = there ? c8 / p.G : 0;
+    uint32_t qa[D / 16][2];                        // [2 j + s]: A registers of the row, first and second half of the 16 elements
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (((size_t)b * p.N + node) * p.Hq + kvh * p.G + (there ? c8 % p.G : 0)) * D) + q4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint4 v = there ? __ldcg(src + 4 * j) : make_uint4(0, 0, 0, 0);
-            qa[2 * j][r] = v.x; qa[2 * j][R + r] = v.y; qa[2 * j + 1][r] = v.z; qa[2 * j + 1][R + r] = v.w;
-        }
-        mk[r][0] = mk[r][1] = 0;
-        if (there) {
-            const uint64_t* mrow = p.mask + ((size_t)b * p.N + node) * W;
-            mk[r][0] = __ldcg(mrow);
-            if (W > 1) mk[r][1] = __ldcg(mrow + 1);
+            qa[2 * j][0] = v.x; qa[2 * j][1] = v.y; qa[2 * j + 1][0] = v.z; qa[2 * j + 1][1] = v.w;
         }
     }
-    float o[16][2 * R], m_ref[R], l_run[R];        // o[t + 8 h][2 r + i]: row c8 + 8 r, element 64 h + 8 (2 q4 + i) + t
+    const uint64_t mk = there ? __ldcg(p.mask + (size_t)b * p.N + node) : 0ull;              // (N <= 8: one word)
+    float o[16][2], m_ref = -INFINITY, l_run = 0.f;                                          // o[t + 8 h][i]: element 64 h + 8 (2 q4 + i) + t
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
-#pragma unroll
-        for (int i = 0; i < 2 * R; ++i) o[t][i] = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) { m_ref[r] = -INFINITY; l_run[r] = 0.f; }
+    for (int t = 0; t < 16; ++t) o[t][0] = o[t][1] = 0.f;
 
     // ---- own keys: groups of 16, number i of this warp is wi + i * nw ----
     const int groups = good && live ? (total + 15) / 16 : 0, mine_n = groups > wi ? (groups - wi + nw - 1) / nw : 0;
@@ -941,42 +927,35 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint4 kk = *reinterpret_cast<const uint4*>(ks + (8 * n + c8) * 256 + (((4 * j + q4) ^ (4 * (c8 & 1))) << 4));
-                const uint32_t a0[4] = {qa[2 * j][0], R > 1 ? qa[2 * j][R - 1] : 0u, qa[2 * j][R], R > 1 ? qa[2 * j][2 * R - 1] : 0u};
-                const uint32_t a1[4] = {qa[2 * j + 1][0], R > 1 ? qa[2 * j + 1][R - 1] : 0u, qa[2 * j + 1][R], R > 1 ? qa[2 * j + 1][2 * R - 1] : 0u};
+                const uint32_t a0[4] = {qa[2 * j][0], 0u, qa[2 * j][1], 0u}, a1[4] = {qa[2 * j + 1][0], 0u, qa[2 * j + 1][1], 0u};
                 mma_16816(sc[n], a0, kk.x, kk.y);
                 mma_16816(sc[n], a1, kk.z, kk.w);
             }
         }
-        uint32_t pr[4] = {0u, 0u, 0u, 0u};
+        float x[4] = {sc[0][0], sc[0][1], sc[1][0], sc[1][1]};                               // keys 2q, 2q+1, 2q+8, 2q+9
+        if (key0 + 16 > S) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float x[4] = {sc[0][2 * r], sc[0][2 * r + 1], sc[1][2 * r], sc[1][2 * r + 1]};   // keys 2q, 2q+1, 2q+8, 2q+9
-            if (key0 + 16 > S) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = key0 + 2 * q4 + (i & 1) + 8 * (i >> 1) - S;               // tree node of this key, if it is one
-                    const uint64_t w = t >= 64 ? mk[r][1] : mk[r][0];
-                    if (t >= 0 && !(t < p.N && (w >> (t & 63)) & 1ull)) x[i] = -INFINITY;
-                }
+            for (int k = 0; k < 4; ++k) {
+                const int t = key0 + 2 * q4 + (k & 1) + 8 * (k >> 1) - S;                   // tree node of this key, if it is one
+                if (t >= 0 && !(t < p.N && (mk >> t) & 1ull)) x[k] = -INFINITY;
             }
-            float top = max_nan(max3_nan(x[0], x[1], x[2]), x[3]);
-            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2)) * p.scale_log2;
-            if (top > m_ref[r] + kRescaleGap) {                                              // also on the first finite group
-                const float a = exp2f(m_ref[r] - top);
-                m_ref[r] = top;
-                l_run[r] *= a;
-#pragma unroll
-                for (int t = 0; t < 16; ++t) { o[t][2 * r] *= a; o[t][2 * r + 1] *= a; }
-            }
-            if (!(top < INFINITY)) l_run[r] = top - top;                                     // a NaN or an infinite score (see inv_sum)
-            const float m_use = m_ref[r] == -INFINITY ? 0.f : m_ref[r];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = exp2f(fmaf(x[i], p.scale_log2, -m_use));
-            l_run[r] += (x[0] + x[1]) + (x[2] + x[3]);                                       // this lane's keys; summed over the lanes below
-            pr[r] = pack_bf16(x[0], x[1]);
-            pr[2 + r] = pack_bf16(x[2], x[3]);
         }
+        float top = max_nan(max3_nan(x[0], x[1], x[2]), x[3]);
+        top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2)) * p.scale_log2;
+        if (top > m_ref + kRescaleGap) {                                                     // also on the first finite group
+            const float a = exp2f(m_ref - top);
+            m_ref = top;
+            l_run *= a;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) { o[t][0] *= a; o[t][1] *= a; }
+        }
+        if (!(top < INFINITY)) l_run = top - top;                                            // a NaN or an infinite score (see inv_sum)
+        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = exp2f(fmaf(x[k], p.scale_log2, -m_use));
+        l_run += (x[0] + x[1]) + (x[2] + x[3]);                                              // this lane's keys; summed over the lanes below
+        const uint32_t pr[4] = {pack_bf16(x[0], x[1]), 0u, pack_bf16(x[2], x[3]), 0u};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint32_t v[4][4];
@@ -988,61 +967,54 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const uint32_t sel = t & 1 ? 0x7632u : 0x5410u;
-                float c[4] = {o[8 * h + t][0], o[8 * h + t][1], R > 1 ? o[8 * h + t][2 * R - 2] : 0.f, R > 1 ? o[8 * h + t][2 * R - 1] : 0.f};
+                float c[4] = {o[8 * h + t][0], o[8 * h + t][1], 0.f, 0.f};
                 mma_16816(c, pr, __byte_perm(v[0][t >> 1], v[1][t >> 1], sel), __byte_perm(v[2][t >> 1], v[3][t >> 1], sel));
                 o[8 * h + t][0] = c[0]; o[8 * h + t][1] = c[1];
-                if (R > 1) { o[8 * h + t][2 * R - 2] = c[2]; o[8 * h + t][2 * R - 1] = c[3]; }
             }
         }
     }
     __syncwarp();                                  // (the stages take the warp's part below)
     // (a NaN or infinite score was seen by all lanes of the row, so every lane's l is NaN then)
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
-        l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 2);
-        if (!(l_run[r] > 0.f)) m_ref[r] = -INFINITY;
-    }
+    l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
+    l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+    if (!(l_run > 0.f)) m_ref = -INFINITY;
 
-    // ---- the prefix's pieces of these rows, from the kernel before ----
+    // ---- the prefix's pieces of the row, from the kernel before ----
     if (p.early && p.P > 0) pdl_wait();
     if (good && live && p.P > 0) {
         const int steps = steps_of(p.P), Rg = range_of(p, p.Hkv * head_places(p, 0, steps)), rows = p.slot_rows[0];
+        const int row = b * RG + min(c8, RG - 1), m = row / kRows, lr = row - m * kRows, nb = p.blocks[0];
+        const bool alt = m == nb - 1 && p.last_alt[0];
+        const int u0 = kvh * head_places(p, 0, steps) + m * unit_places(p, 0, steps, false) + start_places(alt);
+        const int first = u0 / Rg, last = (u0 + (steps - 1) * step_places(alt)) / Rg;
+        const int pieces = last - first + 1;
+        for (int e0 = wi; e0 < pieces; e0 += 2 * nw) {                                       // two at a time, their loads ahead of the sums
+            float2 ml[2];
+            float4 v[2][8];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int row = b * RG + min(c8 + 8 * r, RG - 1), m = row / kRows, lr = row - m * kRows, nb = p.blocks[0];
-            const bool alt = m == nb - 1 && p.last_alt[0];
-            const int u0 = kvh * head_places(p, 0, steps) + m * unit_places(p, 0, steps, false) + start_places(alt);
-            const int first = u0 / Rg, last = (u0 + (steps - 1) * step_places(alt)) / Rg;
-            const int pieces = last - first + 1;
-            for (int e0 = wi; e0 < pieces; e0 += 2 * nw) {                                   // two at a time, their loads ahead of the sums
-                float2 ml[2];
-                float4 v[2][8];
+            for (int k = 0; k < 2; ++k) {
+                const int e = e0 + k * nw < pieces ? e0 + k * nw : e0;
+                const int slot = kvh * nb + m + first + e;
+                ml[k] = __ldcg(p.part_ml[0] + (size_t)slot * rows + lr);
+                const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows + lr;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int e = e0 + k * nw < pieces ? e0 + k * nw : e0;
-                    const int slot = kvh * nb + m + first + e;
-                    ml[k] = __ldcg(p.part_ml[0] + (size_t)slot * rows + lr);
-                    const float4* src = p.part_o[0] + ((size_t)slot * (D / 4) + 4 * q4) * rows + lr;
+                for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows);
+            }
+            if (e0 + nw >= pieces) ml[1] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) v[k][x] = __ldcg(src + (size_t)((x & 3) + 16 * (x >> 2)) * rows);
-                }
-                if (e0 + nw >= pieces) ml[1] = make_float2(-INFINITY, 0.f);
+            for (int k = 0; k < 2; ++k) {
+                const float m_new = fmaxf(m_ref, ml[k].x), m_use = m_new == -INFINITY ? 0.f : m_new;
+                const float a = exp2f(m_ref - m_use), w = exp2f(ml[k].x - m_use);
+                l_run = l_run * a + ml[k].y * w;
+                m_ref = m_new;
+                if (ml[k].x == -INFINITY) continue;                                          // (its o may never have been written)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float m_new = fmaxf(m_ref[r], ml[k].x), m_use = m_new == -INFINITY ? 0.f : m_new;
-                    const float a = exp2f(m_ref[r] - m_use), w = exp2f(ml[k].x - m_use);
-                    l_run[r] = l_run[r] * a + ml[k].y * w;
-                    m_ref[r] = m_new;
-                    if (ml[k].x == -INFINITY) continue;                                      // (its o may never have been written)
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {                                            // elements 64 h + 16 q4 + 4 (x & 3) + 0..3
-                        const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
-                        o[8 * h + t][2 * r + i] = o[8 * h + t][2 * r + i] * a + v[k][x].x * w;
-                        o[8 * h + t + 1][2 * r + i] = o[8 * h + t + 1][2 * r + i] * a + v[k][x].y * w;
-                        o[8 * h + t + 2][2 * r + i] = o[8 * h + t + 2][2 * r + i] * a + v[k][x].z * w;
-                        o[8 * h + t + 3][2 * r + i] = o[8 * h + t + 3][2 * r + i] * a + v[k][x].w * w;
-                    }
+                for (int x = 0; x < 8; ++x) {                                                // elements 64 h + 16 q4 + 4 (x & 3) + 0..3
+                    const int h = x >> 2, i = (x & 3) >> 1, t = 8 * h + 4 * (x & 1);
+                    o[t][i] = o[t][i] * a + v[k][x].x * w;
+                    o[t + 1][i] = o[t + 1][i] * a + v[k][x].y * w;
+                    o[t + 2][i] = o[t + 2][i] * a + v[k][x].z * w;
+                    o[t + 3][i] = o[t + 3][i] * a + v[k][x].w * w;
                 }
             }
         }
@@ -1050,15 +1022,11 @@ few_rows_kernel(const __grid_constant__ PrefixParams p, const __grid_constant__ 
 
     // ---- the warps' parts meet ----
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const int h = x >> 2, i = (x & 3) >> 1, t = 4 * (x & 1);
-            reinterpret_cast<float4*>(mine)[(c8 + 8 * r) * (D / 4 + 1) + 16 * h + 4 * q4 + (x & 3)] =
-                make_float4(o[8 * h + t][2 * r + i], o[8 * h + t + 1][2 * r + i], o[8 * h + t + 2][2 * r + i], o[8 * h + t + 3][2 * r + i]);
-        }
-        if (q4 == 0) park_ml[warp][c8 + 8 * r] = make_float2(m_ref[r], l_run[r]);
+    for (int x = 0; x < 8; ++x) {
+        const int h = x >> 2, i = (x & 3) >> 1, t = 8 * h + 4 * (x & 1);
+        reinterpret_cast<float4*>(mine)[c8 * (D / 4 + 1) + 16 * h + 4 * q4 + (x & 3)] = make_float4(o[t][i], o[t + 1][i], o[t + 2][i], o[t + 3][i]);
     }
+    if (q4 == 0) park_ml[warp][c8] = make_float2(m_ref, l_run);
     if (ck > 1) cluster_sync_all(); else if (wpu > 1) __syncthreads(); else __syncwarp();
     const uint32_t o_at = smem_u32(sm), ml_at = smem_u32(&park_ml[0][0]);
     // thread <-> (row, 4 columns); the ranks of a cluster take rows in turn
@@ -1106,9 +1074,8 @@ struct PrefixLayout {
     long long slots[2];
     size_t bytes[2];
 };
-PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count) {
+PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count, bool alone) {
     PrefixLayout l;
-    const bool alone = N * (Hq / Hkv) <= kFewRows;
     const int G = Hq / Hkv;
     for (int kind = 0; kind < 2; ++kind) {
         l.rows[kind] = (kind ? N : B * N) * G;
@@ -1123,9 +1090,27 @@ PrefixLayout prefix_layout(int B, int N, int Hq, int Hkv, int sm_count) {
 
 }  // namespace
 
+// The larger of what the two ways take where either may be chosen, so that it is never less for more sequences.
 size_t prefix_scratch_bytes(int B, int N, int Hq, int Hkv, int sm_count) {
-    const PrefixLayout l = prefix_layout(B, N, Hq, Hkv, sm_count);
-    return l.bytes[0] + l.bytes[1];
+    const bool few = N * (Hq / Hkv) <= kFewRows;
+    const PrefixLayout line = prefix_layout(few ? std::min(B, kMaxLineB) : B, N, Hq, Hkv, sm_count, false);
+    const PrefixLayout alone = prefix_layout(B, N, Hq, Hkv, sm_count, true);
+    return std::max(line.bytes[0] + line.bytes[1], few ? alone.bytes[0] : 0);
+}
+
+// Keys of its own that a sequence may have, as far as the host can tell.
+static int own_keys(const AttnArgs& a, int prefix) {
+    const int cap = a.S_max - prefix;
+    return a.kv_len_hint > prefix ? std::min(cap, a.kv_len_hint - prefix + a.N) : cap;
+}
+// Do the sequences' own keys go through few_rows_kernel?  Short ones do, and long ones where the prefix outweighs them all; long
+// own keys stream better on the line.  (us, few_rows_kernel / line: 32 x 1 of 40/40 heads on 2880 + 200 keys 47 / 65, 8 x 1 of 28/4 on
+// 3344 + 200 14.2 / 15.3, 8 x 1 of 16/2 on 32768 + 1000 26 / 54; 40 x 1 of 28/4 on 2000 + 2000 46 / 34, 48 x 1 of 32/8 on 1000 + 2000
+// 73 / 69.)
+static bool few_rows(const AttnArgs& a, int prefix) {
+    if (a.N * (a.Hq / a.Hkv) > kFewRows) return false;
+    const int own = own_keys(a, prefix);
+    return a.B > kMaxLineB || own <= 1024 || (long long)a.B * own <= prefix;
 }
 
 cudaError_t init_attn_prefix() {
@@ -1134,20 +1119,17 @@ cudaError_t init_attn_prefix() {
         const cudaError_t e = cudaFuncSetAttribute(m, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
     }
-    for (int r = 1; r <= 2; ++r) {
-        const cudaError_t e = cudaFuncSetAttribute(r == 1 ? (const void*)few_rows_kernel<1> : (const void*)few_rows_kernel<2>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(r));
-        if (e != cudaSuccess) return e;
-    }
+    const cudaError_t f = cudaFuncSetAttribute((const void*)few_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+    if (f != cudaSuccess) return f;
     const cudaError_t e = cudaFuncSetAttribute((const void*)attn_prefix_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
     return e != cudaSuccess ? e : cudaFuncSetAttribute((const void*)attn_prefix_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_ALLOC);
 }
 
 // Sizes that these kernels take: every place of the line and every row of the partials has a 32-bit number.
 bool attn_prefix_supports(const AttnArgs& a, int prefix) {
-    const bool few = a.N * (a.Hq / a.Hkv) <= kFewRows;
+    const bool few = few_rows(a, prefix);
     if ((!few && a.B > kMaxLineB) || !(a.scale > 0.f) || a.D != D || !a.page_rows) return false;
-    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
+    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count, few);
     long long T = 0;
     for (int kind = 0; kind < (few ? 1 : 2); ++kind) {
         const long long steps = ((kind ? (long long)a.S_max - prefix : prefix) + STEP - 1) / STEP;
@@ -1158,7 +1140,8 @@ bool attn_prefix_supports(const AttnArgs& a, int prefix) {
 }
 
 cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cudaStream_t st, int* n_launches) {
-    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count);
+    const bool few = few_rows(a, prefix);
+    const PrefixLayout l = prefix_layout(a.B, a.N, a.Hq, a.Hkv, a.sm_count, few);
     PrefixParams p = {};
     p.q = (const __nv_bfloat16*)a.q; p.kv_len = a.kv_len; p.mask = a.mask;
     p.out = (__nv_bfloat16*)a.out; p.lse = a.lse;
@@ -1176,7 +1159,6 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.status = a.status;
     const PagedArgs pa = {a.block_table, a.table_stride, a.page_rows, a.num_blocks, a.Hkv, a.N, a.token_major, a.status, nullptr};
-    const bool few = l.rows[1] <= kFewRows;
     if (few) {
         p.groups = 0;
         // More SMs than ranges worth having: a unit is cut into equal parts of whole ranges, so that no CTA starts on a second unit
@@ -1196,19 +1178,15 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         ++*n_launches;
     }
     if (few) {
-        // Warps to a unit: as many as the SMs hold at once, as long as each has a group of keys
-        // or a piece of the prefix.
-        const int units = a.B * a.Hkv, steps = steps_of(prefix), T = a.Hkv * head_places(p, 0, steps);
-        const int pieces = steps == 0 ? 0 : unit_places(p, 0, steps, true) / range_of(p, T) + 1, most = std::max((p.cap + 15) / 16, pieces);
-        const int room = (l.rows[1] <= 8 ? 12 : 8) * a.sm_count;
+        // Warps to a unit: as many as the SMs hold at once, as long as each has a group of keys or a piece of the prefix, or in a cluster
+        // four of them (4 x 2 of 32/8 heads on 2000 + 300 keys: 13.4 us with 4 warps, 17.0 with 16; 4 x 1 of 28/4 on 16 + 4000: 55.7, 18.5 with 32).
+        const int units = a.B * a.Hkv, steps = steps_of(prefix), T = a.Hkv * head_places(p, 0, steps), room = 12 * a.sm_count;
+        const int pieces = steps == 0 ? 0 : unit_places(p, 0, steps, true) / range_of(p, T) + 1, most = std::max((own_keys(a, prefix) + 15) / 16, pieces);
         int nw = 1;
-        while (nw < 8 * kFewWarps && 2 * nw <= most && units * 2 * nw <= room) nw *= 2;
+        while (nw < 8 * kFewWarps && (nw < kFewWarps ? 2 : 8) * nw <= most && units * 2 * nw <= room) nw *= 2;
         const int ck = nw > kFewWarps ? nw / kFewWarps : 1, wpu = nw > kFewWarps ? kFewWarps : nw;
         const int blocks = ck > 1 ? units * ck : (units * wpu + kFewWarps - 1) / kFewWarps;
-        auto go = [&](auto kernel, int r) {
-            return launch_pdl(kernel, dim3(blocks), dim3(32 * kFewWarps), few_smem(r), st, ck, p, pa, (const uint4*)a.k, (const uint4*)a.v, wpu);
-        };
-        err = l.rows[1] <= 8 ? go(few_rows_kernel<1>, 1) : go(few_rows_kernel<2>, 2);
+        err = launch_pdl(few_rows_kernel, dim3(blocks), dim3(32 * kFewWarps), kFewSmem, st, ck, p, pa, (const uint4*)a.k, (const uint4*)a.v, wpu);
         if (err == cudaSuccess) ++*n_launches;
         return err;
     }

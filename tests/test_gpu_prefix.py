@@ -113,11 +113,13 @@ CASES = {
     "nothing_shared": (3, 20, 4, 2, 0, [300, 0, 129]),
     "many": (128, 1, 4, 2, 512, [0, 3, 40, 200]),
     "hundreds": (300, 1, 7, 1, 272, [0, 3, 40, 130, 77]),         # prefix rows in nine blocks
-    "few_16_rows": (5, 4, 8, 2, 160, [0, 300, 40, 7, 1000]),      # 16 rows per sequence and kv head
-    "few_rows_blocks": (9, 8, 8, 4, 2000, [5, 0, 333]),           # 16 rows, prefix of 144: 128 and 16
+    "few_8_rows": (5, 2, 8, 2, 160, [0, 300, 40, 7, 900]),        # 8 rows per sequence and kv head
+    "few_9_rows": (5, 3, 6, 2, 160, [0, 300, 40, 7, 900]),
+    "few_rows_blocks": (20, 4, 8, 4, 2000, [5, 0, 333]),          # prefix of 160 rows
     # prefix of 560 rows, two blocks of 256 and one of 48 in alternate steps, each cut into as many parts as a whole block
-    "few_short_last_block": (40, 2, 28, 4, 2000, [300, 5, 0]),
-    "few_wide_last_block": (20, 5, 9, 3, 1500, [30, 5, 0]),       # 300 rows: 256 and 44
+    "few_short_last_block": (80, 1, 28, 4, 2000, [300, 5, 0]),
+    "few_wide_last_block": (50, 2, 9, 3, 1500, [30, 5, 0]),       # 300 rows: 256 and 44
+    "few_long_own": (3, 1, 4, 2, 4096, [1300, 900, 0]),           # own keys in clusters
     "just_above_few": (3, 17, 2, 2, 500, [5, 200, 64]),
     "many_trees": (40, 8, 8, 8, 256, [10, 60, 0, 300, 5]),
     "long_own": (2, 4, 4, 1, 96, [4000, 2500]),
@@ -156,6 +158,17 @@ def test_prefix_lengths_off_the_blocks(P):
         c.call(prefix=less)
         assert c.ctx.status_poll() == 0
         c.check(want=want)
+    c.ctx.close()
+
+
+@pytest.mark.parametrize("hint", [0, 400, 3000, 100000])
+def test_a_hint_steers_the_way_and_not_the_result(hint):
+    """A table with room for far more than the sequences have: the expected length chooses between the ways of reading their own keys."""
+    c = Case(6, 1, 8, 2, 256, [100, 3, 0, 1200], 64, seed=14, cap=8192)
+    c.device(_binding(), option=(_binding().OPT_KV_LEN_HINT, hint))
+    c.call()
+    assert c.ctx.status_poll() == 0
+    c.check()
     c.ctx.close()
 
 
@@ -442,11 +455,11 @@ def test_refusals():
     assert lib.vispec_tree_verify_attn_prefix_paged(z, 0, z, z, z, 1, 0, z, 1, 1, 1.0, z, 0, z, z, z) == E_NULL
     assert ctx.status_poll() == 0
     ctx.close()
-    # more than 16 rows per sequence and kv head: at most 64 sequences
-    big = b.VerifyContext(65, 9, 4, 2, 128, 128, 1)
+    # more than 8 rows per sequence and kv head: at most 64 sequences
+    big = b.VerifyContext(65, 5, 4, 2, 128, 128, 1)
     pool = torch.zeros((8, 2, 16, 128), dtype=torch.bfloat16, device="cuda")
     big.cache_register_paged(0, pool, pool)
-    for N, fine in ((9, False), (8, True)):
+    for N, fine in ((5, False), (4, True)):
         q = torch.zeros((65, N, 4, 128), dtype=torch.bfloat16, device="cuda")
         args = (0, q, torch.zeros(65, dtype=torch.int32, device="cuda"), torch.zeros((65, 8), dtype=torch.int32, device="cuda"), 0,
                 torch.ones((65, N, 1), dtype=torch.int64, device="cuda"), SCALE, big.prefix_scratch(65, N), q.clone())
