@@ -13,17 +13,25 @@
 // cost (a unit's start costs too), and every CTA, one per SM, takes an equal range of it: no case needs a choice of how many SMs
 // the prefix gets, and the device alone knows kv_len.  A CTA's part of a unit is a segment; each segment parks its rows' (m, l, o)
 // in the scratch, and a second kernel adds up a row's pieces.  (A prefix unit and a sequence's unit always have two pieces to
-// add, so there is nothing to gain from finishing a row in the first kernel.)
+// add, so there is nothing to gain from finishing a row in the first kernel.)  With few rows per sequence and kv head, the sequences'
+// own keys are few_rows_kernel's (below), which also joins the pieces, and the prefix is alone on the line.
+//
+// Measured, us of a call among others with changing inputs (floor: bytes at 6516 GB/s or flops at 1652 TFLOP/s):
+//   8 x 128 nodes of 16/2 heads on 32768 shared + 300 to 2048 own keys    271 (173, tensor): 1.06 PFLOP/s
+//   8 x 60 nodes of 32/32 heads on 3904 + 46 to 354                        66 (19.8, tensor)
+//   4 x 60 nodes of 28/4 heads on 3344 + 46 to 354                         26.6 (7.5, tensor)
+//   32 x 1 node of 40/40 heads on 2880 + 46 to 354                         55.5 (29.4, HBM), few rows
+//   8 x 1 node of 28/4 heads on 3344 + 46 to 354                           14.9 (1.6, HBM), few rows: two dependent launches
 //
 // A segment runs on two accumulator tiles of 128 rows, each with four softmax warps, one thread per row, which work out of phase so that
 // the tensor pipe serves one while the other is in its exponentials, as in attn_tc5_wide.cu:
 //   wide        more than 128 rows: the tiles hold different rows and share every K/V stage
-//   alternate   at most 128 rows: both tiles hold the same rows and take turns at the steps; their parts meet at the segment's end
+//   alternate   at most 128 rows: both tiles hold the same rows and take turns at the steps; a row has two parts
 // In terms of "operations" 0, 1, 2, ... (one tile's share of a step; the tiles take turns, across segments too) the issue order is
 // always S(0) S(1) | PV(0) S(2) | PV(1) S(3) | ...
 //
 //   warp 0  producer of the K ring (2 x 32 KB)      warp 2  producer of the V ring (3 x 32 KB)
-//   warp 1  issuer of all products                   warp 3  derives the schedule from kv_len
+//   warp 1  issuer of all products                   warp 3  derives the schedule from kv_len, then fetches alternate segments' Q rows
 //   warps 4-7 / 8-11  softmax of tile A / B: thread <-> TMEM lane <-> query row
 // TMEM (512 columns): S_A 0..127, S_B 128..255 (P of the tile, bf16, in the first 64 columns of its S), O_A 256, O_B 384.
 // The waits, time-outs and the programmatic launch are those of attn_tc5.cu.
@@ -87,6 +95,9 @@ struct PrefixParams {
 
 // Places of the line (some 210 cycles each, from clock stamps of 8 x 60 nodes of 32/32 heads): a wide step 3400 cycles, an alternate
 // one 1900, the start of a segment (Q rows, first score, last product, partials) 7500 and 3500.
+// (Starts of 16 to 36 and 10 to 24 places, alternate steps of 8 to 12: within 5 % of one another on nine shapes, these the best for the
+// longest.)  A range of fewer than kMinRange places costs more to start and to join than it saves: 26 to 36 the same, 44 and 48 6 % more
+// on 8 single tokens of 28/4 heads.
 constexpr int kWideStep = 16, kAltStep = 9, kWideStart = 36, kAltStart = 16, kMinRange = 32;
 __host__ __device__ constexpr int step_places(bool alt) { return alt ? kAltStep : kWideStep; }
 __host__ __device__ constexpr int start_places(bool alt) { return alt ? kAltStart : kWideStart; }
@@ -1190,7 +1201,8 @@ cudaError_t launch_attn_prefix(const AttnArgs& a, int prefix, void* scratch, cud
         if (err == cudaSuccess) ++*n_launches;
         return err;
     }
-    // One group of four columns per thread while that leaves the SMs with few threads, whole 32-byte sectors of the output beyond.
+    // One group of four columns per thread while that leaves the SMs with few threads, whole 32-byte sectors of the output beyond
+    // (8 x 60 nodes of 32/32 heads: 60.9 us, one group each 68.8).
     const long long rows = (long long)a.B * a.N * a.Hq;
     const bool fine = rows * (D / 4) <= 1024ll * a.sm_count;
     const unsigned blocks = (unsigned)((rows * (fine ? D / 4 : D / 16) + 127) / 128);

@@ -3,12 +3,14 @@
 //
 //   x'[j] = x[j] cos a - x[j + D/2] sin a,   x'[j + D/2] = x[j + D/2] cos a + x[j] sin a,   a = positions[axis(j)][t] * theta^(-2j/D)
 //
-// What bounds it: HBM, every row read once and written once; few rows: the chain launch -> positions -> rotation -> store.  So a
-// block forms the D/2 angles of its tokens once and turns all their heads by them, and a thread's first rows are on their way while
-// it does so.  An angle is taken as a number of turns, position times frequency / 2 pi in fp64, whose whole part goes before the
-// rest (half a turn at most) is rounded to fp32: 2^-26 of a turn, the fp64 part less than that up to positions of 2^22; then
-// sine and cosine in fp32, and the products in fp32 with one rounding to bf16.  (Sines in fp64 cost two FP64 warps 400 cycles a
-// token, as much as HBM needs for the 20 rows of a 16/2-head model's token.)
+// What bounds it: HBM, every row read once and written once; few rows: the chain launch -> positions -> rotation -> store.  So a warp
+// forms the D/2 angles of its token once, with its first rows on their way, and turns all the rows it has of the token by them.  An
+// angle is taken as a number of turns, position times frequency / 2 pi in fp64, whose whole part goes before the rest (half a turn at
+// most) is rounded to fp32: 2^-26 of a turn, the fp64 part less than that up to positions of 2^22; then sine and cosine in fp32, and the
+// products in fp32 with one rounding to bf16.  (Sines in fp64 cost two FP64 warps 400 cycles a token, as much as HBM needs for the 20
+// rows of a 16/2-head model's token.)
+// Measured, us of a call among others with changing inputs (floor at 6516 GB/s): 32768 tokens of 16/2 heads rotated 49.6 (46.4), 16000
+// tokens of 40/40 heads appended 160 (151), 3344 of 28/4 rotated 11.0 (8.4) and appended 14.4 (9.5), 8 tokens rotated 2.9, 32 appended 3.5.
 #include <cuda_bf16.h>
 #include <algorithm>
 
