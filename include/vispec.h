@@ -137,7 +137,8 @@ typedef enum vispec_option {
     /* Default 0 (none).  The committed length the caller expects its sequences to have, in slots.  The host never
      * reads kv_len, so where it must choose between ways of running the attention it reasons about the cache
      * capacity S_max; a context sized for 32 k slots that serves 2 k-token sequences is better described by this
-     * hint.  It only steers that choice: any kv_len up to S_max - N stays valid. */
+     * hint.  On a paged layer the capacity is that of a row of the block table.  It only steers that choice: any kv_len up to
+     * S_max - N stays valid. */
     VISPEC_OPT_KV_LEN_HINT = 4,
     /* Default 0 (1 if the environment has VISPEC_DEBUG set at context creation).  vispec_tree_verify_attn also
      * checks its `positions` argument on the device: positions[b][i] == kv_len[b] + (set bits of tree_mask row
@@ -279,6 +280,9 @@ int vispec_tree_verify_attn_paged(vispec_ctx* ctx, int layer, const void* q, con
  *                sequence.  Constant in a captured graph.
  *   scratch      DEVICE, 16-byte aligned, caller-owned, scratch_bytes >= vispec_prefix_scratch_bytes(ctx, B, N): partial results;
  *                nothing in it has to be cleared or kept.  Calls that may overlap on the GPU need scratch of their own.
+ * With at most 8 rows per sequence and kv head (N * Hq / Hkv) the host chooses between two ways of running the sequences' own keys, by
+ * how many they may be: where the table has room for many more than there are, VISPEC_OPT_KV_LEN_HINT should say so (it counts the prefix
+ * too, as kv_len does).
  * kv_len[b] counts the prefix too; a sequence with kv_len[b] below the shared slots or kv_len[b] + N above the table's
  * capacity gets out = 0, lse = -inf and the status word VISPEC_E_RANGE.  No workspace is used.  At most 64 sequences where
  * N * Hq / Hkv > 8; any number up to B_max otherwise.

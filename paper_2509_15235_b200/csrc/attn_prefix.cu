@@ -1109,10 +1109,12 @@ size_t prefix_scratch_bytes(int B, int N, int Hq, int Hkv, int sm_count) {
     return std::max(line.bytes[0] + line.bytes[1], few ? alone.bytes[0] : 0);
 }
 
-// Keys of its own that a sequence may have, as far as the host can tell.
+// Keys of its own that a sequence may have, as far as the host can tell: what the hint says (a committed length, the prefix and all; one
+// below the prefix is none of this call's sequences'), or else all that the table has room for.
 static int own_keys(const AttnArgs& a, int prefix) {
     const int cap = a.S_max - prefix;
-    return a.kv_len_hint > prefix ? std::min(cap, a.kv_len_hint - prefix + a.N) : cap;
+    if (a.kv_len_hint <= 0 || a.kv_len_hint < prefix) return cap;
+    return (int)std::min((long long)cap, (long long)a.kv_len_hint - prefix + a.N);
 }
 // Do the sequences' own keys go through few_rows_kernel?  Short ones do, and long ones where the prefix outweighs them all; long
 // own keys stream better on the line.  (us, few_rows_kernel / line: 32 x 1 of 40/40 heads on 2880 + 200 keys 47 / 65, 8 x 1 of 28/4 on

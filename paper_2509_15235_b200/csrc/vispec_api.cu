@@ -433,6 +433,7 @@ int vispec_tree_verify_attn_prefix_paged(vispec_ctx* c, int layer, const void* q
     a.S_max = table_stride * pr;
     a.scale = scale; a.status = c->d_status; a.sm_count = c->sm_count;
     a.early_prefetch = c->early_prefetch;
+    a.kv_len_hint = c->kv_len_hint;
     a.k_map = &c->k_map[layer]; a.v_map = &c->v_map[layer];
     a.block_table = block_table; a.table_stride = table_stride;
     a.page_rows = pr; a.num_blocks = c->num_blocks[layer]; a.token_major = c->token_major[layer];
