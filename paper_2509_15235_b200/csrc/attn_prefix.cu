@@ -647,8 +647,9 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             if (live) q_ask();
             if (!ok || !(ok = mbar_wait_warp(bar(X_OFULL + x), o_phase, abort_flag))) break;
             float2 ml = make_float2(l_run > 0.f ? m_ref : -INFINITY, l_run);
-            // O is free for the next segment's products as soon as it has been read, ahead of the last stores.  (No partial is read before
-            // this kernel has ended, so the arrival need not wait for them.)
+            // O is free for the next segment's products as soon as it has been read, ahead of the last stores.  (The arrival releases: the
+            // loads from tensor memory are done, tcgen05.wait::ld, and ordered ahead of it.  That it also orders the partials stored
+            // before it cost nothing on the listed shapes.)
             if (ALONE && alt) {
                 // Both tiles have a part of every row; each adds up half of the columns.  (The statistics of the last alternate segment
                 // have been read by everybody: O is complete only after both tiles have let go of the last one's.)
@@ -672,7 +673,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         tmem_ld32(o_addr + from + c * 32, o);
                         tmem_ld32(peer + from + c * 32, q);
                         tmem_wait_ld();
-                        if (c == 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
+                        if (c == 1) { tc_fence_before(); mbar_arrive(bar(X_OFREE + x)); }
                         if (row_ok) {
 #pragma unroll
                             for (int c4 = 0; c4 < 8; ++c4, prow += rows) {
@@ -695,7 +696,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         uint32_t o[32];
                         tmem_ld32(o_addr + c * 32, o);
                         tmem_wait_ld();
-                        if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive_relaxed(bar(X_OFREE + x)); }
+                        if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive(bar(X_OFREE + x)); }
                         if (row_ok && has_o) {                // (without a product the piece has l = 0 and its o is not looked at)
 #pragma unroll
                             for (int c4 = 0; c4 < 8; ++c4, prow += rows)
