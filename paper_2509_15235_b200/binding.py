@@ -306,7 +306,7 @@ class VerifyContext:
 
     def rope_axes_rows(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, axes: RopeAxes,
                        q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor]) -> None:
-        """Rows [T, heads, D] whose tokens may be any stride apart (slices of a fused projection); positions [n_axes, T]."""
+        """Rows [T, heads, D] whose tokens may be any stride apart (slices of a fused projection); positions [n_axes, T], by axis."""
         _check(_native.rope_axes_rows(self._h, *self._heads, q, k, positions, axes._addr, q_out, k_out),
                "vispec_rope_axes_rows")
 

@@ -16,6 +16,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <initializer_list>
+#include <string>
 
 #include "vispec.h"
 
@@ -114,8 +116,26 @@ struct Args {
         r.stride = T > 1 ? t->stride(0) : (int64_t)heads * D;      // (one token: whatever its stride says is not used)
         return r;
     }
-    // A contiguous tensor of `type` and `n` elements on the current device (n < 0: any number).  None: nullptr, where it may be.
-    void* dense(at::ScalarType type, int64_t n, bool optional = false) {
+    // Are the sizes of t those of `want`, or those with neighbours joined or split?  (As many elements in another order of dimensions
+    // are not: every size up to some point has to multiply to the same as some sizes of the other.)
+    static bool fits(const at::Tensor& t, std::initializer_list<int64_t> want) {
+        auto ends_in = [](const int64_t* x, size_t nx, const int64_t* y, size_t ny) {
+            int64_t px = 1, py = 1;
+            for (size_t i = 0, j = 0; i < nx; ++i) {
+                px *= x[i];
+                while (py < px && j < ny) py *= y[j++];
+                if (py != px) return false;
+            }
+            return true;
+        };
+        int64_t n = 1;
+        for (int64_t w : want) n *= w;
+        const auto have = t.sizes();
+        return t.numel() == n && (n == 0 || ends_in(have.data(), have.size(), want.begin(), want.size()) ||
+                                  ends_in(want.begin(), want.size(), have.data(), have.size()));
+    }
+    // A contiguous tensor of `type` and the given sizes on the current device ({}: any).  None: nullptr, where it may be.
+    void* dense(at::ScalarType type, std::initializer_list<int64_t> want, bool optional = false) {
         if (!ok) return nullptr;
         PyObject* o = a[i];
         if (o == Py_None && optional) { ++i; return nullptr; }
@@ -126,16 +146,18 @@ struct Args {
         }
         const at::Tensor& t = THPVariable_Unpack(o);
         if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || t.scalar_type() != type || !t.is_contiguous() ||
-            (n >= 0 && t.numel() != n)) {
-            PyErr_Format(PyExc_ValueError, "a contiguous %s tensor of %lld elements on the current CUDA device is expected",
-                         c10::toString(type), (long long)(n < 0 ? t.numel() : n));
+            (want.size() > 0 && !fits(t, want))) {
+            std::string shape;
+            for (int64_t w : want) shape += (shape.empty() ? "" : ", ") + std::to_string(w);
+            PyErr_Format(PyExc_ValueError, "a contiguous %s tensor of shape [%s] on the current CUDA device is expected",
+                         c10::toString(type), want.size() > 0 ? shape.c_str() : "any");
             ok = false;
             return nullptr;
         }
         ++i;
         return t.data_ptr();
     }
-    int32_t* ints(int64_t n, bool optional = false) { return static_cast<int32_t*>(dense(at::kInt, n, optional)); }
+    int32_t* ints(std::initializer_list<int64_t> want, bool optional = false) { return static_cast<int32_t*>(dense(at::kInt, want, optional)); }
     const vispec_rope_axes* axes() {                                // address of the struct (RopeAxes keeps it), 0: none
         if (!ok) return nullptr;
         void* p = PyLong_AsVoidPtr(a[i++]);
@@ -377,7 +399,7 @@ NATIVE(rope_axes_rows) {
     const vispec_rope_axes* axes = g.axes();
     const auto qo = g.rows(T, Hq, D), ko = g.rows(T, Hkv, D);
     if (g.ok) g.i = 6;
-    auto* pos = g.ints(axes ? axes->n_axes * T : -1);
+    auto* pos = axes ? g.ints({axes->n_axes, T}) : g.ints({});
     return finish(g, [&](void* st) { return vispec_rope_axes_rows(c, q.p, q.stride, k.p, k.stride, pos, (int)T, axes, qo.p, qo.stride, ko.p, ko.stride, st); });
 }
 
@@ -396,22 +418,22 @@ PyObject* kv_append_call(PyObject* const* args, Py_ssize_t nargs) {
     if (g.ok) g.i = 9;
     const vispec_rope_axes* axes = g.axes();
     if (g.ok) g.i = 8;
-    auto* pos = g.ints(axes ? axes->n_axes * T : -1, true);
+    auto* pos = axes ? g.ints({axes->n_axes, T}, true) : g.ints({}, true);
     if (g.ok) g.i = 11;
     const at::Tensor* tl = g.tensor(1);
     const int B = tl ? (int)tl->size(0) : 0;
     if (g.ok) g.i = 10;
-    auto* cu = g.ints(B + 1);
-    auto* kv_len = g.ints(B);
+    auto* cu = g.ints({B + 1});
+    auto* kv_len = g.ints({B});
     int stride = 0;
     int32_t* table = nullptr;
     if (PAGED) {
         const at::Tensor* tt = g.tensor(2);
         stride = tt ? (int)tt->size(1) : 0;
-        table = g.ints((int64_t)B * stride);
+        table = g.ints({B, stride});
     }
     const auto qo = g.rows(T, Hq, D);
-    auto* len_out = g.ints(B, true);
+    auto* len_out = g.ints({B}, true);
     return finish(g, [&](void* st) {
         return PAGED ? vispec_kv_append_paged(c, layer, q.p, q.stride, k.p, k.stride, v.p, v.stride, pos, axes, cu, kv_len, table, stride, B, (int)T, qo.p, qo.stride, len_out, st)
                      : vispec_kv_append(c, layer, q.p, q.stride, k.p, k.stride, v.p, v.stride, pos, axes, cu, kv_len, B, (int)T, qo.p, qo.stride, len_out, st);
@@ -427,19 +449,19 @@ NATIVE(tree_verify_attn_prefix_paged) {
     const int Hq = g.num(), Hkv = g.num(), D = g.num(), layer = g.num();
     (void)Hkv;
     const at::Tensor* t = g.tensor(4);
-    const int64_t B = size(t, 0), N = size(t, 1), all = B * N * Hq;
-    auto* q = g.dense(at::kBFloat16, all * D);
-    auto* kv_len = g.ints(B);
+    const int64_t B = size(t, 0), N = size(t, 1);
+    auto* q = g.dense(at::kBFloat16, {B, N, Hq, D});
+    auto* kv_len = g.ints({B});
     const int stride = size(g.tensor(2), 1);
-    auto* table = g.ints(B * stride);
+    auto* table = g.ints({B, stride});
     const int prefix = g.num();
-    auto* mask = static_cast<uint64_t*>(g.dense(at::kLong, B * N * ((N + 63) / 64)));
+    auto* mask = static_cast<uint64_t*>(g.dense(at::kLong, {B, N, (N + 63) / 64}));
     const float scale = g.real();
     const at::Tensor* ts = g.tensor(1);
-    auto* scratch = g.dense(at::kByte, -1);
+    auto* scratch = g.dense(at::kByte, {});
     const size_t bytes = ts ? (size_t)ts->numel() : 0;
-    auto* out = g.dense(at::kBFloat16, all * D);
-    auto* lse = static_cast<float*>(g.dense(at::kFloat, all, true));
+    auto* out = g.dense(at::kBFloat16, {B, N, Hq, D});
+    auto* lse = static_cast<float*>(g.dense(at::kFloat, {B, Hq, N}, true));
     return finish(g, [&](void* st) { return vispec_tree_verify_attn_prefix_paged(c, layer, q, kv_len, table, stride, prefix, mask, (int)B, (int)N, scale, scratch, bytes, out, lse, st); });
 }
 
