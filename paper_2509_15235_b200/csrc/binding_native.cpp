@@ -89,6 +89,19 @@ struct Args {
         }
         return static_cast<T*>(t.data_ptr());
     }
+    // A tensor's memory, which has to be on the current device.  Looked at in this order: a fake tensor has neither memory nor,
+    // maybe, a device, and its address of zero would pass for an argument that is not given.
+    void* memory(const at::Tensor& t) {
+        void* const p = t.data_ptr();
+        if (!p && t.numel() > 0) {
+            PyErr_SetString(PyExc_RuntimeError, "a tensor has no storage");
+            ok = false;
+        } else if (t.get_device() != c10::cuda::current_device()) {
+            PyErr_SetString(PyExc_ValueError, "tensors must be on the current CUDA device");
+            ok = false;
+        }
+        return p;
+    }
     // [T, heads, D] bf16 on the current device, a token's heads contiguous, tokens any number of elements apart.  T < 0: the
     // tensor's own count is taken over, otherwise it has to be T.  None: nullptr.
     struct Rows { void* p = nullptr; int64_t stride = 0; };
@@ -99,8 +112,8 @@ struct Args {
         const at::Tensor* t = tensor(3);
         if (!t) return r;
         ++i;
-        if (!t->is_cuda() || t->get_device() != c10::cuda::current_device() || t->scalar_type() != at::kBFloat16) {
-            PyErr_SetString(PyExc_ValueError, "rows must be bfloat16 on the current CUDA device");
+        if (!t->is_cuda() || t->scalar_type() != at::kBFloat16) {
+            PyErr_SetString(PyExc_ValueError, "rows must be bfloat16 CUDA tensors");
             ok = false;
         } else if ((T >= 0 && t->size(0) != T) || t->size(1) != heads || t->size(2) != D) {
             PyErr_Format(PyExc_ValueError, "rows of %lld tokens, %d heads and head size %d are expected", (long long)(T < 0 ? t->size(0) : T), heads, D);
@@ -112,7 +125,7 @@ struct Args {
         if (!ok) return r;
         if (t->size(0) > INT_MAX) { PyErr_SetString(PyExc_ValueError, "too many tokens"); ok = false; return r; }
         T = t->size(0);
-        r.p = t->data_ptr();
+        r.p = memory(*t);
         r.stride = T > 1 ? t->stride(0) : (int64_t)heads * D;      // (one token: whatever its stride says is not used)
         return r;
     }
@@ -145,17 +158,17 @@ struct Args {
             return nullptr;
         }
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || t.scalar_type() != type || !t.is_contiguous() ||
+        if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous() ||
             (want.size() > 0 && !fits(t, want))) {
             std::string shape;
             for (int64_t w : want) shape += (shape.empty() ? "" : ", ") + std::to_string(w);
-            PyErr_Format(PyExc_ValueError, "a contiguous %s tensor of shape [%s] on the current CUDA device is expected",
+            PyErr_Format(PyExc_ValueError, "a contiguous %s CUDA tensor of shape [%s] is expected",
                          c10::toString(type), want.size() > 0 ? shape.c_str() : "any");
             ok = false;
             return nullptr;
         }
         ++i;
-        return t.data_ptr();
+        return memory(t);
     }
     int32_t* ints(std::initializer_list<int64_t> want, bool optional = false) { return static_cast<int32_t*>(dense(at::kInt, want, optional)); }
     const vispec_rope_axes* axes() {                                // address of the struct (RopeAxes keeps it), 0: none

@@ -2,6 +2,8 @@
 import glob
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 
@@ -16,3 +18,47 @@ def test_barriers_are_arrived_at_with_release():
     assert sources
     for path in sources:
         assert not re.search(r"mbarrier\.arrive[.\w]*\.relaxed", open(path).read()), path
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2509_15235_b200 import binding, build
+    build.build()
+    return binding.load()
+
+
+# every tensor of the type and shape that the call takes
+CALLS = [
+    "rope_axes_rows(0, 4, 2, 128, q, None, pos, ax._addr, q, None)",
+    "rope_axes_rows(0, 4, 2, 128, None, k, pos, ax._addr, None, k)",
+    "kv_append(0, 4, 2, 128, 0, q, k, k, pos, ax._addr, cu, kv, q, kv)",
+    "kv_append_paged(0, 4, 2, 128, 0, q, k, k, pos, ax._addr, cu, kv, table, q, kv)",
+    "tree_verify_attn_prefix_paged(0, 4, 2, 128, 0, tree, kv, table, 0, mask, 1.0, scratch, tree, lse)",
+]
+
+
+def test_tensors_without_storage_are_refused(lib):
+    """A fake CUDA tensor has no memory: whichever the binding meets first it names, before anything asks for a device, and instead of
+    passing on an address of zero (which an optional argument would take for "not given")."""
+    code = f"""
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+from paper_2509_15235_b200 import binding
+binding.load()
+ax = binding.RopeAxes((64,), 1e4)
+with FakeTensorMode():
+    t = lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, device="cuda", dtype=dtype)
+    q, k, tree, pos = t(1, 4, 128), t(1, 2, 128), t(1, 1, 4, 128), t(1, 1, dtype=torch.int32)
+    cu, kv, table = t(2, dtype=torch.int32), t(1, dtype=torch.int32), t(1, 8, dtype=torch.int32)
+    mask, scratch, lse = t(1, 1, 1, dtype=torch.int64), t(64, dtype=torch.uint8), t(1, 4, 1, dtype=torch.float32)
+for call in {CALLS!r}:
+    try:
+        eval("binding._native." + call)
+        print("nothing raised", call)
+    except RuntimeError as e:
+        print("raised", str(e).splitlines()[0])
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=300)
+    said = r.stdout.splitlines()
+    assert r.returncode == 0 and len(said) == len(CALLS), (r.returncode, r.stderr[-500:])
+    assert all(s.startswith("raised") and "storage" in s for s in said), said
