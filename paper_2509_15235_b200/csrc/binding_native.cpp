@@ -45,7 +45,12 @@ struct Args {
     int num() {
         if (!ok) return 0;
         const long v = PyLong_AsLong(a[i++]);
-        if (v == -1 && PyErr_Occurred()) ok = false;
+        if (v == -1 && PyErr_Occurred()) {
+            ok = false;
+        } else if (v < INT_MIN || v > INT_MAX) {
+            PyErr_SetString(PyExc_OverflowError, "an integer of 32 bits is expected");
+            ok = false;
+        }
         return static_cast<int>(v);
     }
     float real() {

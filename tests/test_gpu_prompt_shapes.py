@@ -96,3 +96,20 @@ def test_prefix_tensors_in_another_order_are_refused(N):
         assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
     assert ctx.status_poll() == 0
     ctx.close()
+
+
+def test_integers_beyond_the_calls_own_are_refused():
+    """2^32 + 64 is not a prefix of 64."""
+    c = Case(2, 1, 4, 2, 64, [30, 7], 16, seed=2)
+    ctx = c.device(_binding())
+    for P in (2 ** 32 + 64, 2 ** 31, -2 ** 31 - 1, 2 ** 64):
+        with pytest.raises(OverflowError):
+            c.call(prefix=P)
+    with pytest.raises(OverflowError):
+        ctx.tree_verify_attn_prefix_paged(2 ** 32, c.qd, c.kvd, c.td, 64, c.md, 1.0, c.scratch, c.out, c.lse)
+    with pytest.raises(_binding().VispecError):
+        c.call(prefix=2 ** 31 - 1)
+    c.call()
+    c.check()
+    assert ctx.status_poll() == 0
+    ctx.close()

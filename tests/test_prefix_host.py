@@ -62,3 +62,15 @@ for call in {CALLS!r}:
     said = r.stdout.splitlines()
     assert r.returncode == 0 and len(said) == len(CALLS), (r.returncode, r.stderr[-500:])
     assert all(s.startswith("raised") and "storage" in s for s in said), said
+
+
+@pytest.mark.parametrize("call", ["tree_verify_attn_prefix_paged(0, 4, 2, 128, {}, None, None, None, 0, None, 1.0, None, None, None)",
+                                  "kv_append(0, 4, 2, 128, {}, None, None, None, None, 0, None, None, None, None)",
+                                  "rope_axes_rows(0, {}, 2, 128, None, None, None, 0, None, None)",
+                                  "tree_verify_attn(0, {}, None, None, None, None, None, None, 1.0, None, None)"])
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32, 2 ** 63 - 1, 2 ** 64, -2 ** 31 - 1])
+def test_integers_beyond_an_int_are_refused(lib, call, value):
+    """2^32 is not layer 0."""
+    from paper_2509_15235_b200 import binding
+    with pytest.raises(OverflowError):
+        eval("binding._native." + call.format(value))
