@@ -59,3 +59,26 @@ def kernels_of(fn):
         res = fn()
         torch.cuda.synchronize()
     return res, {e.key for e in prof.key_averages()}
+
+
+def kernels_captured(fn):
+    """The names (mangled) of the kernels that fn launches on the current stream.  fn is captured into a graph that never runs; unlike a
+    profile, a graph loses none."""
+    from cuda.bindings import driver
+
+    def done(answer):
+        assert answer[0] == driver.CUresult.CUDA_SUCCESS, answer[0]
+        return answer[1]
+
+    captured = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(captured):
+        fn()
+    graph = driver.CUgraph(captured.raw_cuda_graph())
+    count = driver.cuGraphGetNodes(graph)[2]
+    names = set()
+    for node in done(driver.cuGraphGetNodes(graph, count)):
+        if done(driver.cuGraphNodeGetType(node)) == driver.CUgraphNodeType.CU_GRAPH_NODE_TYPE_KERNEL:
+            params = done(driver.cuGraphKernelNodeGetParams(node))
+            name = done(driver.cuFuncGetName(params.func) if int(params.func) else driver.cuKernelGetName(params.kern))
+            names.add(name.decode())
+    return names

@@ -17,9 +17,10 @@ pytestmark = pytest.mark.gpu
 def test_the_hint_chooses_the_way_and_leaves_the_result(P, hint, few):
     c = Case(6, 1, 8, 2, P, [100, 3, 0, 1200], 64, seed=14, cap=8192)
     c.device(_binding(), option=(_binding().OPT_KV_LEN_HINT, hint))
-    _, names = gu.kernels_of(c.call)
+    names = gu.kernels_captured(c.call)
     assert any("few_rows_kernel" in n for n in names) == few, names
     assert any("prefix_merge_kernel" in n for n in names) != few, names
+    c.call()
     assert c.ctx.status_poll() == 0
     c.check()
     c.ctx.close()
@@ -29,12 +30,12 @@ def test_the_hint_chooses_the_way_and_leaves_the_result(P, hint, few):
 def test_a_hint_given_between_calls_counts_from_the_next_one(hint):
     c = Case(3, 2, 8, 4, 128, [700, 0, 90], 16, seed=15, cap=4096)
     c.device(_binding())
-    first, names = gu.kernels_of(lambda: (c.call(), c.out.clone())[1])
-    assert not any("few_rows_kernel" in n for n in names)
+    assert not any("few_rows_kernel" in n for n in gu.kernels_captured(c.call))
+    c.call()
     c.ctx.ctx_set_option(_binding().OPT_KV_LEN_HINT, hint)
     c.out.fill_(float("nan"))
-    _, names = gu.kernels_of(c.call)
-    assert any("few_rows_kernel" in n for n in names) == (hint == 300)
+    assert any("few_rows_kernel" in n for n in gu.kernels_captured(c.call)) == (hint == 300)
+    c.call()
     assert c.ctx.status_poll() == 0
     c.check()
     c.ctx.close()
