@@ -273,7 +273,11 @@ int vispec_tree_verify_attn_paged(vispec_ctx* ctx, int layer, const void* q, con
 /* Attention of a batch whose sequences share a prefix (several samples, questions or drafts behind one image or video, Sec. 5.3's
  * thousands of image tokens), on a paged layer: the result of vispec_tree_verify_attn_paged (up to the order of its sums) for
  * sequences whose block tables start with the same blocks, with the prefix read once instead of once per sequence.  N = 1 is
- * single-token decoding.  Arguments as there, and:
+ * single-token decoding.  What it saves is (B - 1) * Hkv * prefix_len rows of keys; what it costs is a second kernel and the pieces
+ * that go between the two, 4 to 8 us in short calls.  From some 260,000 rows on, with a prefix of four times a sequence's own keys and
+ * nodes or more, it was the faster call on every shape measured, 1.1 to 6 times; below that it depends on the shape, and for few
+ * sequences, few kv heads or prefixes of hundreds vispec_tree_verify_attn_paged is mostly the faster one, by up to a factor of two.
+ * Arguments as there, and:
  *   prefix_len   host: the first prefix_len slots are held by the same blocks for all B sequences, i.e. the first
  *                floor(prefix_len / page_rows) entries of every row of block_table are those of row 0, the only row whose entries
  *                are read there.  0: nothing is shared.  Slots of a block that prefix_len ends within are looked up per

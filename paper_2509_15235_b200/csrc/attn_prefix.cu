@@ -11,16 +11,17 @@
 // Work.  Two kinds of units: (kv head, block of 256 of the batch's B*N*G rows) over the prefix, and (sequence, kv head, block of 256
 // of its N*G rows) over its own keys, both in steps of 128 keys.  All steps lie on one line, the prefix units first, each with its
 // cost (a unit's start costs too), and every CTA, one per SM, takes an equal range of it: no case needs a choice of how many SMs
-// the prefix gets, and the device alone knows kv_len.  A CTA's part of a unit is a segment; each segment parks its rows' (m, l, o)
+// the prefix gets, and kv_len, which the device alone knows, decides.  A CTA's part of a unit is a segment; each segment parks its rows' (m, l, o)
 // in the scratch, and a second kernel adds up a row's pieces.  (A prefix unit and a sequence's unit always have two pieces to
 // add, so there is nothing to gain from finishing a row in the first kernel.)  With few rows per sequence and kv head, the sequences'
-// own keys are few_rows_kernel's (below), which also joins the pieces, and the prefix is alone on the line.
+// own keys are few_rows_kernel's (below), which also joins the pieces, and the prefix is alone on the line.  That, and what goes with it (the cut
+// of the prefix's units, warps and clusters per unit), the host chooses, by the lengths that it has to expect (own_keys).
 //
 // Measured, us of a call among others with changing inputs (floor: bytes at 6516 GB/s or flops at 1652 TFLOP/s):
-//   8 x 128 nodes of 16/2 heads on 32768 shared + 300 to 2048 own keys    271 (173, tensor): 1.06 PFLOP/s
+//   8 x 128 nodes of 16/2 heads on 32768 shared + 300 to 2048 own keys    275 (173, tensor): 1.04 PFLOP/s
 //   8 x 60 nodes of 32/32 heads on 3904 + 46 to 354                        66 (19.8, tensor)
-//   4 x 60 nodes of 28/4 heads on 3344 + 46 to 354                         26.6 (7.5, tensor)
-//   32 x 1 node of 40/40 heads on 2880 + 46 to 354                         55.5 (29.4, HBM), few rows
+//   4 x 60 nodes of 28/4 heads on 3344 + 46 to 354                         27.1 (7.5, tensor)
+//   32 x 1 node of 40/40 heads on 2880 + 46 to 354                         55.7 (29.4, HBM), few rows
 //   8 x 1 node of 28/4 heads on 3344 + 46 to 354                           14.9 (1.6, HBM), few rows: two dependent launches
 //
 // A segment runs on two accumulator tiles of 128 rows, each with four softmax warps, one thread per row, which work out of phase so that
@@ -829,7 +830,7 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
 //
 // What bounds it: the read of the own keys.  A tile of 128 rows would be nearly empty and its segments would cost more to start than
 // to stream (32 sequences x 40 heads with one row each: 8 segments per SM of 8 to 10 thousand cycles), so here a warp takes 16 keys at
-// a time on its own, by asynchronous 16-byte copies into shared memory of its own, a group ahead, and has nothing to set up:
+// a time on its own, by asynchronous 16-byte copies into shared memory of its own, a group ahead, and has no barrier to set up:
 //   S = Q K^T   (mma.sync m16n8k16) lane (key k = lane / 4, part q = lane % 4) reads 16 bytes of key k at elements 32 j + 8 q: the pairs
 //               are the B operand of two products whose 16 contracted elements are 32 j + 8 q' + 4 s + {0, 1} and + {2, 3}; Q alike.
 //   O += P V    P is S's accumulator layout read as an A operand.  The lane reads 16 bytes of keys 2q, 2q + 1, 2q + 8, 2q + 9 at
@@ -837,7 +838,9 @@ prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
 //               consecutive elements of each half of its rows.
 // (Loaded straight into registers instead, 12 warps of 168 registers per SM reached 3.7 TB/s: a warp then either loads or computes.)
 // A unit is a warp's, or that of 2 or 4 warps of a block, or where units are few of a cluster of 2, 4 or 8 blocks; they take the groups
-// of 16 keys and the prefix's pieces in turn, their (m, l, o) meet in shared memory and the row is finished here.
+// of 16 keys and the prefix's pieces in turn, their (m, l, o) meet in shared memory, behind a barrier of the block or two of the
+// cluster, and the row is finished here.  (Three blocks per SM leave 168 registers a thread; the assembler spills 36 bytes, in the
+// join of the prefix's pieces.)
 // ------------------------------------------------------------------------------------------------
 constexpr int kFewWarps = 4, kFewRows = 8, kFewStages = 2;
 constexpr int kFewStage = 2 * 16 * D * 2;          // bytes of 16 keys and their values
@@ -1118,9 +1121,15 @@ static int own_keys(const AttnArgs& a, int prefix) {
     return (int)std::min((long long)cap, (long long)a.kv_len_hint - prefix + a.N);
 }
 // Do the sequences' own keys go through few_rows_kernel?  Short ones do, and long ones where the prefix outweighs them all; long
-// own keys stream better on the line.  (us, few_rows_kernel / line: 32 x 1 of 40/40 heads on 2880 + 200 keys 47 / 65, 8 x 1 of 28/4 on
-// 3344 + 200 14.2 / 15.3, 8 x 1 of 16/2 on 32768 + 1000 26 / 54; 40 x 1 of 28/4 on 2000 + 2000 46 / 34, 48 x 1 of 32/8 on 1000 + 2000
-// 73 / 69.)
+// own keys stream better on the line.  us, few_rows_kernel / line, sequences x nodes of heads on prefix + own keys:
+//   won   32 x 1 of 40/40 on 2880 + 200     47.4 / 66.7    2 x 1 of 40/40 on 2880 + 200   22.9 / 27.4    24 x 1 of 32/8 on 3000 + 100  16.5 / 18.9
+//         8 x 1 of 28/4 on 3344 + 200       14.6 / 15.6    32 x 1 of 28/4 on 3344 + 200   19.0 / 19.4    8 x 1 of 32/32 on 2000 + 500  29.7 / 30.9
+//         8 x 1 of 16/2 on 32768 + 1000     28.1 / 54.2
+//   lost  2 x 1 of 28/4 on 1000 + 100       13.2 / 10.7    2 x 8 of 32/32 on 3000 + 300   25.0 / 19.9    20 x 1 of 16/2 on 2000 + 300  14.1 / 13.3
+//         4 x 2 of 32/8 on 2000 + 300       13.7 / 13.2    4 x 1 of 32/8 on 1000 + 800    13.9 / 13.1    8 x 4 of 32/32 on 3000 + 300  28.1 / 26.8
+//         16 x 1 of 32/32 on 2000 + 500     44.0 / 43.5    16 x 8 of 32/32 on 3000 + 300  44.1 / 43.2
+//   longer own keys (an earlier form of this kernel): 40 x 1 of 28/4 on 2000 + 2000 46 / 34, 48 x 1 of 32/8 on 1000 + 2000 73 / 69
+// The rule knows the lengths only, so calls of few units are up to a quarter slower than they could be.
 static bool few_rows(const AttnArgs& a, int prefix) {
     if (a.N * (a.Hq / a.Hkv) > kFewRows) return false;
     const int own = own_keys(a, prefix);

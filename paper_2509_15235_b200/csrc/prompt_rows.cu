@@ -9,8 +9,9 @@
 // most) is rounded to fp32: 2^-26 of a turn, the fp64 part less than that up to positions of 2^22; then sine and cosine in fp32, and the
 // products in fp32 with one rounding to bf16.  (Sines in fp64 cost two FP64 warps 400 cycles a token, as much as HBM needs for the 20
 // rows of a 16/2-head model's token.)
-// Measured, us of a call among others with changing inputs (floor at 6516 GB/s): 32768 tokens of 16/2 heads rotated 49.6 (46.4), 16000
-// tokens of 40/40 heads appended 160 (151), 3344 of 28/4 rotated 11.0 (8.4) and appended 14.4 (9.5), 8 tokens rotated 2.9, 32 appended 3.5.
+// Measured, us of a call among others with changing inputs (floor at 6516 GB/s): 32768 tokens of 16/2 heads rotated 48.7 (46.4), 16000
+// tokens of 40/40 heads appended 160 (151), 3344 of 28/4 rotated 11.1 (8.4) and appended 14.5 (9.5), 8 tokens rotated 2.9, 32 appended 3.5.
+// Head size 64, back to back: 32768 tokens of 16/2 heads rotated 28.7 (23.2), 16000 of 40/40 appended 82 (75).
 #include <cuda_bf16.h>
 #include <algorithm>
 
